@@ -541,6 +541,114 @@ tp_status tp_tree_advantage(const int32_t* parent, int32_t n_nodes, const int32_
                             int32_t n_out, float* adv, double* stats, void* workspace, int64_t workspace_bytes,
                             void* cuda_stream);
 
+/* ---- a policy's logits ---------------------------------------------------
+ * Between the attention above and the sampler's branch split, and between the
+ * tree advantage and a training step, lie operators on the logits that the
+ * caller's model gives each token: the log probabilities that tp_branch_assign
+ * takes (Sec. 4.6), their gradient, the clipped policy-gradient loss that the
+ * advantages of Eq. tree_ae are for, and distillation from a teacher's top
+ * logits. Every call takes rows of `vocab` logits; with
+ *   x_j = logit_j / temperature,  LSE = ln sum_j exp(x_j),
+ *   p_j = exp(x_j - LSE),         H = -sum_j p_j ln p_j.
+ *
+ * All pointers are device pointers; calls are asynchronous on cuda_stream, need
+ * no workspace and may be captured into a CUDA graph. n == 0 is a no-op. Sums are
+ * held in fp32 and are the same from run to run; probabilities below 2^-126 count
+ * as 0. Edges, in every call:
+ *   - a negative token id marks a padding row: its logits are not read, its
+ *     outputs (and gradient) are 0;
+ *   - a token id >= vocab makes the row's log probability, loss and gradient NaN
+ *     (nothing out of range is read);
+ *   - a logit of -infinity (a token that is not allowed) has p = 0; a row of
+ *     nothing else has log probability -inf, H = 0, LSE = -inf and gradient 0;
+ *   - a row that holds NaN or +infinity has NaN for all of its results.
+ * Errors (tp_last_error(NULL)): TP_ERR_INVALID_ARG, TP_ERR_CUDA.
+ */
+#define TP_BF16 0
+#define TP_F16 1
+#define TP_F32 2
+#define TP_MAX_VOCAB 393216
+#define TP_MAX_ALTERNATIVES 128
+#define TP_MAX_TEACHER_LOGITS 512
+
+/* A batch of rows of logits.
+ *   data: device, aligned to its elements; row i starts at element
+ *       i * row_stride (row_stride >= vocab). Rows need no other alignment.
+ *   n: rows, 0 .. 2^27. vocab: 1 .. TP_MAX_VOCAB. dtype: TP_BF16, TP_F16 or
+ *       TP_F32. temperature: 1e-4 .. 1e4. */
+typedef struct {
+    const void* data;
+    int64_t row_stride;
+    int32_t n;
+    int32_t vocab;
+    int32_t dtype;
+    float temperature;
+} tp_logits;
+
+/*
+ * Log probabilities of given tokens, with the entropy and the top alternatives
+ * (scoring of sampled segments, Sec. 4.6; a teacher's answers; the choices of a
+ * decode step). tokens: int32 [n], or NULL where there are none yet (then logp
+ * must be NULL and no row is padding). logp = x_token - LSE, entropy = H, lse: fp32 [n], each may be
+ * NULL. k > 0: top_ids int32 [n][k] and top_logp fp32 [n][k] receive the k most
+ * probable tokens in descending order, of equal logits the lower id first;
+ * places that no token with p > 0 in exact arithmetic (a logit above -inf) is
+ * left for hold id -1 and -inf, and so do padding rows; a row with NaN or +inf
+ * has ids -1 and NaN. 0 <= k <= min(vocab, TP_MAX_ALTERNATIVES).
+ */
+tp_status tp_token_logprobs(const tp_logits* logits, const int32_t* tokens, float* logp, float* entropy, float* lse,
+                            int32_t k, int32_t* top_ids, float* top_logp, void* cuda_stream);
+
+/*
+ * Gradient of the log probabilities and entropies with respect to the logits,
+ * from tp_token_logprobs' lse (and entropy):
+ *   dlogits_j = (dlogp (1[j = token] - p_j) - dentropy p_j (ln p_j + H)) / temperature.
+ * dlogp, dentropy: fp32 [n]; one of the two may be NULL. tokens: int32 [n]; NULL
+ * only without dlogp. entropy: fp32 [n], NULL only without dentropy. dlogits:
+ * rows of the logits' type, grad_stride elements apart; it may be the logits
+ * themselves (same address and stride), else it must not overlap them.
+ */
+tp_status tp_token_logprobs_backward(const tp_logits* logits, const int32_t* tokens, const float* lse,
+                                     const float* entropy, const float* dlogp, const float* dentropy, void* dlogits,
+                                     int64_t grad_stride, void* cuda_stream);
+
+/*
+ * Clipped policy-gradient loss of sampled tokens and its gradient, in one pass
+ * over the logits. Row i, with ratio r = exp(logp - old_logp) (1 where old_logp
+ * is NULL: the step is on-policy) and advantage A (tp_tree_advantage's, of the
+ * token's trajectory):
+ *   loss = weight (-min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) - entropy_coef H)
+ *   dlogits_j = weight / temperature (g (1[j = token] - p_j) + entropy_coef p_j (ln p_j + H)),
+ *   g = 0 where the clip holds (A > 0 and r > 1 + clip_high, or A < 0 and
+ *   r < 1 - clip_low) or A = 0 (the first term of the loss is 0 then), else -r A.
+ * A batch's loss is the sum of its rows' (weight: fp32 [n], 1 where NULL). loss
+ * fp32 [n]; logp, entropy: fp32 [n] or NULL. dlogits: NULL for the loss alone,
+ * else as in tp_token_logprobs_backward. A row of -inf logits only has gradient 0.
+ * 0 <= clip_low <= 1, clip_high >= 0, entropy_coef finite.
+ */
+tp_status tp_policy_loss(const tp_logits* logits, const int32_t* tokens, const float* advantage, const float* old_logp,
+                         const float* weight, float clip_low, float clip_high, float entropy_coef, float* loss,
+                         float* logp, float* entropy, void* dlogits, int64_t grad_stride, void* cuda_stream);
+
+/*
+ * Distillation from a teacher's top logits and its gradient, in one pass over
+ * the logits. teacher_ids: int32 [n][k] (distinct in a row, in any order; a
+ * negative id is an empty place; if an id does come twice its shares add up),
+ * teacher_logits: [n][k] of teacher_dtype, logits or log probabilities (top_ids
+ * and top_logp of tp_token_logprobs are such a pair). With q = softmax of the
+ * row's teacher logits / temperature:
+ *   loss = weight sum_k q_k (ln q_k - ln p_{id_k}),
+ *   dlogits_j = weight / temperature (p_j - sum_{k: id_k = j} q_k).
+ * A row without a teacher logit above -inf is padding (loss and gradient 0, its
+ * logits are not read); an id >= vocab with a share, NaN or +inf among them make it NaN. loss
+ * fp32 [n]; it is +inf where a token with a share has p = 0 (the gradient is
+ * still finite). weight: fp32 [n], 1 where NULL. dlogits: NULL for the loss
+ * alone, else as in tp_token_logprobs_backward. 1 <= k <= TP_MAX_TEACHER_LOGITS.
+ */
+tp_status tp_distill_loss(const tp_logits* logits, const int32_t* teacher_ids, const void* teacher_logits,
+                          int32_t teacher_dtype, int32_t k, const float* weight, float* loss, void* dlogits,
+                          int64_t grad_stride, void* cuda_stream);
+
 /* ---- inspection (tests and tools) ------------------------------------ */
 
 /* Pool slot of every token on leaf's root-to-leaf path (its trajectory

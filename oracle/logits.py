@@ -1,0 +1,123 @@
+"""fp64 oracle of the operators on a policy's logits (include/treepo.h): rows of
+logits, x = logits / temperature, p = softmax(x), H its entropy. NumPy, one row
+at a time, from the formulas."""
+import numpy as np
+
+
+def _row(logits, temperature):
+    """(ln p, p, H, lse) of one row; (None, ...) where it holds NaN or +inf."""
+    x = np.asarray(logits, np.float64) / np.float64(temperature)
+    if np.isnan(x).any() or (x == np.inf).any():
+        nan = np.full(x.shape, np.nan)
+        return nan, nan, np.nan, np.nan
+    m = x.max()
+    if m == -np.inf:
+        return np.full(x.shape, -np.inf), np.zeros(x.shape), 0.0, -np.inf
+    lse = m + np.log(np.exp(x - m).sum())
+    lp = (x - m) - np.log(np.exp(x - m).sum())
+    p = np.exp(lp)
+    some = p > 0
+    return lp, p, -(p[some] * lp[some]).sum(), lse
+
+
+def _p_log_p_plus(p, lp, h):
+    """p (ln p + h), 0 where p = 0."""
+    out = np.where(np.isnan(p), np.nan, 0.0)
+    some = p > 0
+    out[some] = p[some] * (lp[some] + h)
+    return out
+
+
+def token_logprobs(logits, tokens, temperature=1.0, k=0):
+    n, v = logits.shape
+    logp, entropy, lse = np.zeros(n), np.zeros(n), np.zeros(n)
+    ids, top = np.full((n, k), -1, np.int64), np.full((n, k), -np.inf)
+    for i in range(n):
+        if tokens is not None and tokens[i] < 0:
+            continue
+        lp, _, entropy[i], lse[i] = _row(logits[i], temperature)
+        if tokens is not None:
+            logp[i] = lp[tokens[i]] if tokens[i] < v else np.nan
+        if k and np.isnan(lse[i]):
+            top[i] = np.nan
+        elif k:
+            x = np.asarray(logits[i], np.float64) + 0.0  # -0 and +0 are equal
+            order = np.lexsort((np.arange(v), -x))[:k]
+            some = x[order] > -np.inf
+            ids[i, : some.sum()] = order[some]
+            top[i, : some.sum()] = lp[order[some]]
+    return dict(logp=logp, entropy=entropy, lse=lse, top_ids=ids, top_logp=top)
+
+
+def token_logprobs_backward(logits, tokens, lse, entropy, dlogp, dentropy, temperature=1.0):
+    n, v = logits.shape
+    out = np.zeros((n, v))
+    for i in range(n):
+        if tokens is not None and tokens[i] < 0:
+            continue
+        if lse[i] == -np.inf:
+            out[i] = np.nan if dlogp is not None and tokens[i] >= v else 0.0
+            continue
+        lp = np.asarray(logits[i], np.float64) / temperature - np.float64(lse[i])
+        p = np.exp(lp)
+        if dlogp is not None:
+            out[i] -= dlogp[i] * p
+            if tokens[i] < v:
+                out[i, tokens[i]] += dlogp[i]
+            else:
+                out[i] = np.nan
+        if dentropy is not None:
+            out[i] -= dentropy[i] * _p_log_p_plus(p, lp, np.float64(entropy[i]))
+    return out / temperature
+
+
+def policy_loss(logits, tokens, advantage, old_logp=None, weight=None, clip_low=0.2, clip_high=0.2, entropy_coef=0.0,
+                temperature=1.0):
+    n, v = logits.shape
+    loss, logp, entropy, grad = np.zeros(n), np.zeros(n), np.zeros(n), np.zeros((n, v))
+    for i in range(n):
+        if tokens[i] < 0:
+            continue
+        w = 1.0 if weight is None else np.float64(weight[i])
+        lp, p, entropy[i], _ = _row(logits[i], temperature)
+        logp[i] = lp[tokens[i]] if tokens[i] < v else np.nan
+        a = np.float64(advantage[i])
+        r = 1.0 if old_logp is None else np.exp(logp[i] - np.float64(old_logp[i]))
+        g = term = 0.0
+        if np.isnan(logp[i]) or np.isnan(r) or np.isnan(a):
+            g = term = np.nan
+        elif a != 0:
+            term = -min(r * a, min(max(r, 1 - clip_low), 1 + clip_high) * a)
+            clipped = (a > 0 and r > 1 + clip_high) or (a < 0 and r < 1 - clip_low)
+            g = 0.0 if clipped else -r * a
+        loss[i] = w * (term - entropy_coef * entropy[i])
+        if np.isnan(g):
+            grad[i] = np.nan
+        elif (p > 0).any():
+            d = -g * p
+            d[tokens[i]] += g
+            grad[i] = w / temperature * (d + entropy_coef * _p_log_p_plus(p, lp, entropy[i]))
+    return dict(loss=loss, logp=logp, entropy=entropy, dlogits=grad)
+
+
+def distill_loss(logits, ids, teacher, weight=None, temperature=1.0):
+    n, v = logits.shape
+    loss, grad = np.zeros(n), np.zeros((n, v))
+    for i in range(n):
+        w = 1.0 if weight is None else np.float64(weight[i])
+        t = np.asarray(teacher[i], np.float64)[ids[i] >= 0] / temperature
+        at = ids[i][ids[i] >= 0]
+        if not len(t) or (t == -np.inf).all():
+            continue
+        lq, q, _, _ = _row(t, 1.0)
+        lp, p, _, lse = _row(logits[i], temperature)
+        if np.isnan(q).any() or np.isnan(lse) or (at[q > 0] >= v).any():
+            loss[i] = grad[i] = np.nan
+            continue
+        at, q, lq = at[q > 0], q[q > 0], lq[q > 0]
+        loss[i] = w * (q * (lq - lp[at])).sum()
+        if (p > 0).any():
+            d = p.copy()
+            np.add.at(d, at, -q)
+            grad[i] = w / temperature * d
+    return dict(loss=loss, dlogits=grad)

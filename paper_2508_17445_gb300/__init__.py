@@ -27,6 +27,8 @@ __all__ = [
     "tp_rollout", "tp_advantage_workspace_bytes", "tp_tree_advantage", "tp_prefill", "tp_debug_prefill_schedule", "tp_decode_host", "tp_prefill_host", "tp_debug_wait_probe", "TpRolloutParams", "TpRolloutStats",
     "TpRolloutProbe", "rollout_params", "TP_BRANCH_EVEN", "TP_BRANCH_LOGP_HIGH", "TP_BRANCH_LOGP_LOW",
     "EVENT_NAMES", "TP_SEG_EOS", "TP_SEG_BOXED", "TP_SEG_FAILED", "TP_SEG_MAX_DEPTH", "Forest", "TP_DECODE_NO_SHARE", "TP_DECODE_CUDA_CORE_SMALL", "TP_DECODE_NO_CACHE", "TP_DECODE_TCGEN05", "TP_DECODE_ALL_TCGEN05", "TP_MMA_SYNC",
+    "tp_token_logprobs", "tp_token_logprobs_backward", "tp_policy_loss", "tp_distill_loss", "TpLogits", "TP_MAX_VOCAB",
+    "TP_MAX_ALTERNATIVES", "TP_MAX_TEACHER_LOGITS",
     "EXPORTED_SYMBOLS",
 ]
 
@@ -50,6 +52,11 @@ TP_BRANCH_LOGP_LOW = 2
 TP_SEG_EOS, TP_SEG_BOXED, TP_SEG_FAILED, TP_SEG_MAX_DEPTH = 1, 2, 4, 8
 EVENT_NAMES = {1: "root", 2: "fork", 3: "segment", 4: "output", 5: "prune", 6: "fallback", 7: "done"}
 
+TP_BF16, TP_F16, TP_F32 = 0, 1, 2
+TP_MAX_VOCAB = 393216
+TP_MAX_ALTERNATIVES = 128
+TP_MAX_TEACHER_LOGITS = 512
+
 STATUS_NAMES = {0: "OK", -1: "INVALID_ARG", -2: "OOM", -3: "BAD_NODE", -4: "FROZEN", -5: "NOT_LEAF",
                 -6: "EMPTY_PATH", -7: "CUDA", -8: "DEVICE"}
 
@@ -60,7 +67,8 @@ EXPORTED_SYMBOLS = (
     "tp_debug_gather", "tp_debug_schedule", "tp_decode_noalloc", "tp_append_tokens", "tp_synth_tokens",
     "tp_branch_assign", "tp_rollout", "tp_advantage_workspace_bytes", "tp_tree_advantage", "tp_prefill",
     "tp_debug_prefill_schedule", "tp_decode_host", "tp_prefill_host", "tp_debug_wait_probe",
-    "tp_debug_check_schedule",
+    "tp_debug_check_schedule", "tp_token_logprobs", "tp_token_logprobs_backward", "tp_policy_loss",
+    "tp_distill_loss",
 )
 
 
@@ -115,6 +123,11 @@ class TpStats(ctypes.Structure):
                 ("live_nodes", ctypes.c_int64), ("total_nodes", ctypes.c_int64)]
 
 
+class TpLogits(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("n", ctypes.c_int32),
+                ("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32), ("temperature", ctypes.c_float)]
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -130,6 +143,7 @@ def load_library() -> ctypes.CDLL:
                           "(there is no fallback implementation)")
     lib = ctypes.CDLL(_LIB_PATH)
     P, I32, I64, U32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint32
+    F32 = ctypes.c_float
     sig = {
         "tp_pool_bytes": (I64, [P]),
         "tp_tree_create": (I32, [P, P]),
@@ -163,6 +177,10 @@ def load_library() -> ctypes.CDLL:
         "tp_debug_wait_probe": (I32, [P, I64]),
         "tp_debug_prefill_schedule": (I32, [P, P, P, I32, U32, P, I64, P]),
         "tp_debug_check_schedule": (I32, [P, P, I64, P]),
+        "tp_token_logprobs": (I32, [P, P, P, P, P, I32, P, P, P]),
+        "tp_token_logprobs_backward": (I32, [P, P, P, P, P, P, P, I64, P]),
+        "tp_policy_loss": (I32, [P, P, P, P, P, F32, F32, F32, P, P, P, P, I64, P]),
+        "tp_distill_loss": (I32, [P, P, P, I32, I32, P, P, P, I64, P]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -454,6 +472,131 @@ def tp_tree_advantage(parent, leaf, reward, adv, stats=None, workspace=None, str
                                           int(leaf.shape[0]), _ptr(adv), _ptr(stats), _ptr(workspace),
                                           int(workspace.numel()), stream)
     _check(None, st)
+
+
+# ---------------------------------------------------- a policy's logits --
+_INT32 = 3
+_dtype_codes: Dict = {}  # torch dtype -> TP_BF16 / TP_F16 / TP_F32, _INT32
+
+
+def _code(t) -> int:
+    if not _dtype_codes:
+        import torch
+        _dtype_codes.update({torch.bfloat16: TP_BF16, torch.float16: TP_F16, torch.float32: TP_F32, torch.int32: _INT32})
+    return _dtype_codes.get(t.dtype, -1)
+
+
+def _float_code(t) -> int:
+    c = _code(t)
+    if c < 0 or c == _INT32:
+        raise ValueError(f"bf16, fp16 or fp32 expected, not {t.dtype}")
+    return c
+
+
+def _rows(t, n: int, vocab: int, code: int, device) -> int:
+    """Elements between the rows of [n][vocab] tensor ``t``."""
+    if t.dim() != 2 or t.shape[0] != n or t.shape[1] != vocab or _code(t) != code or t.device != device:
+        raise ValueError("dlogits must have the logits' shape, type and device")
+    s = t.stride()
+    if s[1] != 1 and vocab > 1:
+        raise ValueError("the elements of a row must be contiguous")
+    return s[0] if n > 1 else max(s[0], vocab)
+
+
+def _logits(t, temperature: float) -> TpLogits:
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError("logits must be a CUDA tensor of shape [n][vocab]")
+    n, v = t.shape
+    code = _float_code(t)
+    return TpLogits(t.data_ptr(), _rows(t, n, v, code, t.device) if v else 0, n, v, code, temperature)
+
+
+def _row_values(t, name: str, shape, device, int32: bool = False):
+    """Pointer of a contiguous fp32 (int32) tensor of this shape, or None."""
+    if t is None:
+        return None
+    if t.shape != shape or t.device != device or not t.is_contiguous() or _code(t) != (_INT32 if int32 else TP_F32):
+        raise ValueError(f"{name} must be a contiguous {'int32' if int32 else 'fp32'} tensor {list(shape)} on the logits' device")
+    return t.data_ptr()
+
+
+def _stream_of(t, stream) -> int:
+    if stream is not None:
+        return getattr(stream, "cuda_stream", stream)
+    import torch
+    return torch.cuda.current_stream(t.device).cuda_stream
+
+
+def tp_token_logprobs(logits, tokens=None, logp=None, entropy=None, lse=None, top_ids=None, top_logp=None,
+                      temperature: float = 1.0, stream=None) -> None:
+    """logits: bf16, fp16 or fp32 [n][vocab] on the device (rows may lie apart); tokens int32 [n]; logp, entropy, lse
+    fp32 [n] or None; top_ids int32 [n][k] and top_logp fp32 [n][k] or None. Runs on ``stream`` (a torch stream or a
+    raw handle), by default torch's current stream."""
+    view = _logits(logits, temperature)
+    n, dev = view.n, logits.device
+    k = 0
+    if top_ids is not None or top_logp is not None:
+        if top_ids is None or top_logp is None or top_ids.dim() != 2:
+            raise ValueError("top_ids and top_logp come together, [n][k]")
+        k = int(top_ids.shape[1])
+    st = load_library().tp_token_logprobs(
+        ctypes.byref(view), _row_values(tokens, "tokens", (n,), dev, True), _row_values(logp, "logp", (n,), dev),
+        _row_values(entropy, "entropy", (n,), dev), _row_values(lse, "lse", (n,), dev), k,
+        _row_values(top_ids, "top_ids", (n, k), dev, True), _row_values(top_logp, "top_logp", (n, k), dev),
+        _stream_of(logits, stream))
+    if st:
+        _check(None, st)
+
+
+def tp_token_logprobs_backward(logits, tokens, lse, dlogits, dlogp=None, dentropy=None, entropy=None,
+                               temperature: float = 1.0, stream=None) -> None:
+    """dlogits: the logits' shape and type (it may be the logits); lse, entropy: tp_token_logprobs' results; dlogp,
+    dentropy: fp32 [n], one may be None."""
+    view = _logits(logits, temperature)
+    n, dev = view.n, logits.device
+    st = load_library().tp_token_logprobs_backward(
+        ctypes.byref(view), _row_values(tokens, "tokens", (n,), dev, True), _row_values(lse, "lse", (n,), dev),
+        _row_values(entropy, "entropy", (n,), dev), _row_values(dlogp, "dlogp", (n,), dev),
+        _row_values(dentropy, "dentropy", (n,), dev), _ptr(dlogits),
+        _rows(dlogits, n, view.vocab, view.dtype, dev), _stream_of(logits, stream))
+    if st:
+        _check(None, st)
+
+
+def tp_policy_loss(logits, tokens, advantage, loss, dlogits=None, old_logp=None, weight=None, logp=None, entropy=None,
+                   clip_low: float = 0.2, clip_high: float = 0.2, entropy_coef: float = 0.0, temperature: float = 1.0,
+                   stream=None) -> None:
+    """tokens int32 [n]; advantage, old_logp, weight, loss, logp, entropy fp32 [n] (all but advantage and loss may be
+    None); dlogits: the logits' shape and type (it may be the logits) or None."""
+    view = _logits(logits, temperature)
+    n, dev = view.n, logits.device
+    st = load_library().tp_policy_loss(
+        ctypes.byref(view), _row_values(tokens, "tokens", (n,), dev, True),
+        _row_values(advantage, "advantage", (n,), dev), _row_values(old_logp, "old_logp", (n,), dev),
+        _row_values(weight, "weight", (n,), dev), clip_low, clip_high, entropy_coef, _row_values(loss, "loss", (n,), dev),
+        _row_values(logp, "logp", (n,), dev), _row_values(entropy, "entropy", (n,), dev), _ptr(dlogits),
+        0 if dlogits is None else _rows(dlogits, n, view.vocab, view.dtype, dev), _stream_of(logits, stream))
+    if st:
+        _check(None, st)
+
+
+def tp_distill_loss(logits, teacher_ids, teacher_logits, loss, dlogits=None, weight=None, temperature: float = 1.0,
+                    stream=None) -> None:
+    """teacher_ids int32 [n][k], teacher_logits bf16, fp16 or fp32 [n][k]; loss, weight fp32 [n] (weight may be None);
+    dlogits: the logits' shape and type (it may be the logits) or None."""
+    view = _logits(logits, temperature)
+    n, dev = view.n, logits.device
+    if teacher_ids.dim() != 2 or teacher_logits.shape != teacher_ids.shape or teacher_logits.device != dev or \
+            not teacher_logits.is_contiguous():
+        raise ValueError("teacher_ids and teacher_logits must be contiguous [n][k] tensors on the logits' device")
+    k = int(teacher_ids.shape[1])
+    st = load_library().tp_distill_loss(
+        ctypes.byref(view), _row_values(teacher_ids, "teacher_ids", (n, k), dev, True), teacher_logits.data_ptr(),
+        _float_code(teacher_logits), k, _row_values(weight, "weight", (n,), dev), _row_values(loss, "loss", (n,), dev),
+        _ptr(dlogits), 0 if dlogits is None else _rows(dlogits, n, view.vocab, view.dtype, dev),
+        _stream_of(logits, stream))
+    if st:
+        _check(None, st)
 
 
 # ------------------------------------------------------------------ owner --

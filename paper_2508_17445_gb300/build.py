@@ -25,7 +25,7 @@ LIB = os.path.join(HERE, "libtreepo.so")
 LIB_CHECKED = os.path.join(HERE, "libtreepo_checked.so")
 BUILD_DIR = os.path.join(HERE, "_build")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
-SOURCES = ["kernels.cu", "forest.cpp", "capi.cpp", "rollout.cpp"]
+SOURCES = ["kernels.cu", "logits.cu", "forest.cpp", "capi.cpp", "rollout.cpp"]
 
 
 def _nvcc() -> str:

@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 #include <new>
 #include <string>
 
@@ -9,6 +10,7 @@
 #include <nvtx3/nvToolsExt.h>
 
 #include "forest.h"
+#include "logits.h"
 
 using tp::fail;
 
@@ -590,6 +592,158 @@ tp_status tp_tree_advantage(const int32_t* parent, int32_t n_nodes, const int32_
         return TP_ERR_CUDA;
     }
     return TP_OK;
+}
+
+namespace {
+
+// Errors of the calls without a tree; a message that finds no memory is left out.
+tp_status bad_arg(const char* m) noexcept {
+    try {
+        g_create_err = m;
+    } catch (...) {
+        g_create_err.clear();
+    }
+    return TP_ERR_INVALID_ARG;
+}
+
+tp_status kernel_status(cudaError_t e, const char* what) noexcept {
+    if (e == cudaSuccess) return TP_OK;
+    try {
+        g_create_err = std::string(what) + ": " + cudaGetErrorString(e);
+    } catch (...) {
+        g_create_err.clear();
+    }
+    return TP_ERR_CUDA;
+}
+
+// The checks of a batch of rows; fills what every operator takes. dx: the
+// gradient's rows (has_dx: some are written).
+tp_status take_logits(const tp_logits* l, const void* dx, int64_t dx_stride, bool has_dx, tp::RowArgs& a) {
+    if (!l) return bad_arg("logits must be non-NULL");
+    if (l->n < 0 || l->n > (1 << 27)) return bad_arg("n must lie in [0, 2^27]");
+    if (l->vocab < 1 || l->vocab > TP_MAX_VOCAB) return bad_arg("vocab must lie in [1, TP_MAX_VOCAB]");
+    if (l->dtype != TP_BF16 && l->dtype != TP_F16 && l->dtype != TP_F32) return bad_arg("dtype must be TP_BF16, TP_F16 or TP_F32");
+    if (!(l->temperature >= 1e-4f && l->temperature <= 1e4f)) return bad_arg("temperature must lie in [1e-4, 1e4]");
+    constexpr int64_t kMaxStride = 1ll << 33;  // times 2^27 rows of 4 bytes stays below 2^63
+    if (l->row_stride < l->vocab || l->row_stride > kMaxStride) return bad_arg("row_stride must be at least vocab (and at most 2^33)");
+    const size_t size = l->dtype == TP_F32 ? 4 : 2;
+    if (l->n > 0 && (!l->data || !aligned(l->data, size))) return bad_arg("logits data must be non-NULL and aligned to its elements");
+    if (has_dx) {
+        if (dx_stride < l->vocab || dx_stride > kMaxStride) return bad_arg("grad_stride must be at least vocab (and at most 2^33)");
+        if (l->n > 0 && (!dx || !aligned(dx, size))) return bad_arg("dlogits must be non-NULL and aligned to its elements");
+        if (l->n > 0) {
+            const uintptr_t x0 = (uintptr_t)l->data, x1 = x0 + ((l->n - 1) * l->row_stride + l->vocab) * size;
+            const uintptr_t d0 = (uintptr_t)dx, d1 = d0 + ((l->n - 1) * dx_stride + l->vocab) * size;
+            if (x0 < d1 && d0 < x1 && !(x0 == d0 && (l->row_stride == dx_stride || l->n == 1)))
+                return bad_arg("dlogits must be the logits themselves (same address and stride) or not overlap them");
+        }
+    }
+    a.x = l->data;
+    a.x_stride = l->row_stride;
+    a.dx = has_dx ? const_cast<void*>(dx) : nullptr;
+    a.dx_stride = dx_stride;
+    a.n = l->n;
+    a.vocab = l->vocab;
+    a.dtype = l->dtype;
+    a.temperature = l->temperature;
+    return TP_OK;
+}
+
+bool words_ok(std::initializer_list<const void*> v) {
+    for (const void* p : v)
+        if (p && !aligned(p, 4)) return false;
+    return true;
+}
+
+constexpr char kWords[] = "fp32 and int32 arrays must be 4-byte aligned";
+
+}  // namespace
+
+tp_status tp_token_logprobs(const tp_logits* logits, const int32_t* tokens, float* logp, float* entropy, float* lse,
+                            int32_t k, int32_t* top_ids, float* top_logp, void* cuda_stream) {
+    tp::CallRange range("tp_token_logprobs");
+    tp::RowArgs a{};
+    if (tp_status st = take_logits(logits, nullptr, 0, false, a); st != TP_OK) return st;
+    if (k < 0 || k > TP_MAX_ALTERNATIVES || k > a.vocab) return bad_arg("k must lie in [0, min(vocab, TP_MAX_ALTERNATIVES)]");
+    if (logp && !tokens) return bad_arg("logp needs tokens");
+    if (k > 0 && a.n > 0 && (!top_ids || !top_logp)) return bad_arg("k > 0 needs top_ids and top_logp");
+    if (!words_ok({tokens, logp, entropy, lse, top_ids, top_logp})) return bad_arg(kWords);
+    a.tokens = tokens;
+    a.logp = logp;
+    a.entropy = entropy;
+    a.lse = lse;
+    a.k = k;
+    a.top_ids = top_ids;
+    a.top_logp = top_logp;
+    if (a.n == 0) return TP_OK;
+    return kernel_status(tp::launch_token_logprobs(a, (cudaStream_t)cuda_stream), "token_logprobs kernel");
+}
+
+tp_status tp_token_logprobs_backward(const tp_logits* logits, const int32_t* tokens, const float* lse,
+                                     const float* entropy, const float* dlogp, const float* dentropy, void* dlogits,
+                                     int64_t grad_stride, void* cuda_stream) {
+    tp::CallRange range("tp_token_logprobs_backward");
+    tp::RowArgs a{};
+    if (tp_status st = take_logits(logits, dlogits, grad_stride, true, a); st != TP_OK) return st;
+    if (!dlogp && !dentropy) return bad_arg("one of dlogp and dentropy must be given");
+    if (dlogp && !tokens) return bad_arg("dlogp needs tokens");
+    if (dentropy && !entropy) return bad_arg("dentropy needs entropy");
+    if (a.n > 0 && !lse) return bad_arg("lse must be non-NULL");
+    if (!words_ok({tokens, lse, entropy, dlogp, dentropy})) return bad_arg(kWords);
+    a.tokens = tokens;
+    a.lse_in = lse;
+    a.entropy_in = entropy;
+    a.dlogp = dlogp;
+    a.dentropy = dentropy;
+    if (a.n == 0) return TP_OK;
+    return kernel_status(tp::launch_token_logprobs_backward(a, (cudaStream_t)cuda_stream), "token_logprobs_backward kernel");
+}
+
+tp_status tp_policy_loss(const tp_logits* logits, const int32_t* tokens, const float* advantage, const float* old_logp,
+                         const float* weight, float clip_low, float clip_high, float entropy_coef, float* loss,
+                         float* logp, float* entropy, void* dlogits, int64_t grad_stride, void* cuda_stream) {
+    tp::CallRange range("tp_policy_loss");
+    tp::RowArgs a{};
+    if (tp_status st = take_logits(logits, dlogits, grad_stride, dlogits != nullptr, a); st != TP_OK) return st;
+    if (!(clip_low >= 0.f && clip_low <= 1.f)) return bad_arg("clip_low must lie in [0, 1]");
+    if (!(clip_high >= 0.f) || !std::isfinite(clip_high)) return bad_arg("clip_high must be finite and >= 0");
+    if (!std::isfinite(entropy_coef)) return bad_arg("entropy_coef must be finite");
+    if (a.n > 0 && (!tokens || !advantage || !loss)) return bad_arg("tokens, advantage and loss must be non-NULL");
+    if (!words_ok({tokens, advantage, old_logp, weight, loss, logp, entropy})) return bad_arg(kWords);
+    a.tokens = tokens;
+    a.advantage = advantage;
+    a.old_logp = old_logp;
+    a.weight = weight;
+    a.clip_low = clip_low;
+    a.clip_high = clip_high;
+    a.entropy_coef = entropy_coef;
+    a.loss = loss;
+    a.logp = logp;
+    a.entropy = entropy;
+    if (a.n == 0) return TP_OK;
+    return kernel_status(tp::launch_policy_loss(a, (cudaStream_t)cuda_stream), "policy_loss kernel");
+}
+
+tp_status tp_distill_loss(const tp_logits* logits, const int32_t* teacher_ids, const void* teacher_logits,
+                          int32_t teacher_dtype, int32_t k, const float* weight, float* loss, void* dlogits,
+                          int64_t grad_stride, void* cuda_stream) {
+    tp::CallRange range("tp_distill_loss");
+    tp::RowArgs a{};
+    if (tp_status st = take_logits(logits, dlogits, grad_stride, dlogits != nullptr, a); st != TP_OK) return st;
+    if (k < 1 || k > TP_MAX_TEACHER_LOGITS) return bad_arg("k must lie in [1, TP_MAX_TEACHER_LOGITS]");
+    if (teacher_dtype != TP_BF16 && teacher_dtype != TP_F16 && teacher_dtype != TP_F32)
+        return bad_arg("teacher_dtype must be TP_BF16, TP_F16 or TP_F32");
+    if (a.n > 0 && (!teacher_ids || !teacher_logits || !loss)) return bad_arg("teacher_ids, teacher_logits and loss must be non-NULL");
+    if (!words_ok({teacher_ids, weight, loss}) || (teacher_logits && !aligned(teacher_logits, teacher_dtype == TP_F32 ? 4 : 2)))
+        return bad_arg("fp32 and int32 arrays must be 4-byte aligned, teacher_logits to its elements");
+    a.teacher_ids = teacher_ids;
+    a.teacher_logits = teacher_logits;
+    a.teacher_dtype = teacher_dtype;
+    a.k = k;
+    a.weight = weight;
+    a.loss = loss;
+    if (a.n == 0) return TP_OK;
+    return kernel_status(tp::launch_distill_loss(a, (cudaStream_t)cuda_stream), "distill_loss kernel");
 }
 
 tp_status tp_fork(tp_tree* t, tp_node node, int32_t k, tp_node* out_children) {

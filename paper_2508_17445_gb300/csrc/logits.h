@@ -1,0 +1,48 @@
+// logits.h -- operators on a policy's logits: what the entry points
+// (capi.cpp) hand to the kernels (logits.cu).
+#ifndef TREEPO_LOGITS_H_
+#define TREEPO_LOGITS_H_
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "treepo.h"
+
+namespace tp {
+
+// One call; each operator uses its own part (see treepo.h). n > 0, arguments checked.
+struct RowArgs {
+    const void* x;          // [n][x_stride] of dtype
+    void* dx;               // [n][dx_stride] of dtype, or null
+    int64_t x_stride, dx_stride;
+    int32_t n, vocab, dtype;
+    float temperature;
+    const int32_t* tokens;  // [n], < 0: padding
+    float* logp;            // [n] outputs, each may be null (loss: where there is one, never)
+    float* entropy;
+    float* lse;
+    float* loss;
+    int32_t k;              // alternatives, or teacher logits a row
+    int32_t* top_ids;       // [n][k]
+    float* top_logp;
+    const float* lse_in;    // [n] of the forward pass
+    const float* entropy_in;
+    const float* dlogp;
+    const float* dentropy;
+    const float* advantage; // [n]
+    const float* old_logp;  // [n] or null
+    const float* weight;    // [n] or null
+    float clip_low, clip_high, entropy_coef;
+    const int32_t* teacher_ids;  // [n][k], < 0: empty
+    const void* teacher_logits;  // [n][k] of teacher_dtype
+    int32_t teacher_dtype;
+};
+
+cudaError_t launch_token_logprobs(const RowArgs& a, cudaStream_t s);
+cudaError_t launch_token_logprobs_backward(const RowArgs& a, cudaStream_t s);
+cudaError_t launch_policy_loss(const RowArgs& a, cudaStream_t s);
+cudaError_t launch_distill_loss(const RowArgs& a, cudaStream_t s);
+
+}  // namespace tp
+
+#endif  // TREEPO_LOGITS_H_

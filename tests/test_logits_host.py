@@ -1,0 +1,166 @@
+"""Operators on a policy's logits, without a GPU: what the entry points refuse
+(before anything is launched), and the fp64 oracle's gradients against
+differences of its losses."""
+import ctypes
+
+import numpy as np
+import pytest
+
+import oracle.logits as L
+import paper_2508_17445_gb300 as tp
+
+A16 = 1 << 20  # a pointer that is never followed: every call here is refused, or has no rows
+FAR = 1 << 40
+
+
+def view(**kw):
+    d = dict(data=A16, row_stride=1000, n=4, vocab=1000, dtype=0, temperature=1.0)
+    d.update(kw)
+    return ctypes.byref(tp.TpLogits(*[d[f] for f, _ in tp.TpLogits._fields_]))
+
+
+def logprobs(l=None, tokens=A16, logp=A16, entropy=A16, lse=A16, k=0, ids=None, top=None):
+    return tp.load_library().tp_token_logprobs(l if l is not None else view(), tokens, logp, entropy, lse, k, ids, top, None)
+
+
+def backward(l=None, tokens=A16, lse=A16, entropy=A16, dlogp=A16, dentropy=A16, dx=FAR, stride=1000):
+    return tp.load_library().tp_token_logprobs_backward(l if l is not None else view(), tokens, lse, entropy, dlogp, dentropy,
+                                                        dx, stride, None)
+
+
+def policy(l=None, tokens=A16, adv=A16, old=A16, weight=A16, lo=0.2, hi=0.2, beta=0.0, loss=A16, logp=A16, entropy=A16,
+           dx=FAR, stride=1000):
+    return tp.load_library().tp_policy_loss(l if l is not None else view(), tokens, adv, old, weight, lo, hi, beta, loss, logp,
+                                            entropy, dx, stride, None)
+
+
+def distill(l=None, ids=A16, teacher=A16, dtype=2, k=4, weight=A16, loss=A16, dx=FAR, stride=1000):
+    return tp.load_library().tp_distill_loss(l if l is not None else view(), ids, teacher, dtype, k, weight, loss, dx, stride, None)
+
+
+CALLS = [logprobs, backward, policy, distill]
+BAD_VIEWS = [dict(n=-1), dict(n=(1 << 27) + 1), dict(vocab=0), dict(vocab=tp.TP_MAX_VOCAB + 1, row_stride=1 << 20), dict(dtype=3),
+             dict(dtype=-1), dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=float("nan")),
+             dict(temperature=float("inf")), dict(temperature=1e-5), dict(row_stride=999), dict(row_stride=0),
+             dict(row_stride=-1000), dict(row_stride=(1 << 33) + 1), dict(data=None), dict(data=A16 + 1), dict(data=A16 + 2, dtype=2)]
+
+
+@pytest.mark.parametrize("call", CALLS)
+@pytest.mark.parametrize("bad", BAD_VIEWS, ids=str)
+def test_bad_rows_are_refused(call, bad):
+    assert call(view(**bad)) == -1
+    assert tp.tp_last_error(None)
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_null_view_and_no_rows(call):
+    assert call(ctypes.c_void_p()) == -1
+    assert "non-NULL" in tp.tp_last_error(None)
+    assert call(view(n=0, data=None)) == 0
+
+
+@pytest.mark.parametrize("kw", [dict(tokens=None), dict(k=-1), dict(k=129, ids=A16, top=A16), dict(k=5), dict(k=5, ids=A16),
+                                dict(k=5, top=A16), dict(tokens=A16 + 2), dict(logp=A16 + 1), dict(lse=A16 + 2),
+                                dict(k=1, ids=A16 + 2, top=A16)], ids=str)
+def test_token_logprobs_refuses(kw):
+    assert logprobs(**kw) == -1
+
+
+def test_more_alternatives_than_tokens():
+    assert logprobs(view(vocab=7), k=8, ids=A16, top=A16) == -1
+    assert "vocab" in tp.tp_last_error(None)
+
+
+BAD_GRADIENTS = [dict(stride=999), dict(stride=-1), dict(dx=FAR + 1),
+                 dict(dx=A16, stride=1001),     # the logits' own memory with other rows
+                 dict(dx=A16 + 2),              # shifted into the logits
+                 dict(dx=A16 + 2 * 3999),       # its first element is the logits' last
+                 dict(dx=A16 - 2 * 3999)]
+
+
+@pytest.mark.parametrize("call", [backward, policy, distill])
+@pytest.mark.parametrize("kw", BAD_GRADIENTS, ids=str)
+def test_bad_gradient_rows_are_refused(call, kw):
+    assert call(**kw) == -1
+
+
+@pytest.mark.parametrize("kw", [dict(dx=None), dict(lse=None), dict(dlogp=None, dentropy=None), dict(tokens=None),
+                                dict(entropy=None), dict(dlogp=A16 + 2)], ids=str)
+def test_backward_refuses(kw):
+    assert backward(**kw) == -1
+
+
+@pytest.mark.parametrize("kw", [dict(tokens=None), dict(adv=None), dict(loss=None), dict(lo=-0.1), dict(lo=1.5), dict(hi=-0.1),
+                                dict(lo=float("nan")), dict(hi=float("inf")), dict(beta=float("nan")), dict(beta=float("inf")),
+                                dict(weight=A16 + 2)], ids=str)
+def test_policy_loss_refuses(kw):
+    assert policy(**kw) == -1
+
+
+@pytest.mark.parametrize("kw", [dict(ids=None), dict(teacher=None), dict(loss=None), dict(k=0), dict(k=513), dict(dtype=3),
+                                dict(dtype=-1), dict(teacher=A16 + 2), dict(teacher=A16 + 1, dtype=0), dict(ids=A16 + 1)], ids=str)
+def test_distill_loss_refuses(kw):
+    assert distill(**kw) == -1
+
+
+def test_binding_refuses_host_tensors():
+    torch = pytest.importorskip("torch")
+    x, one = torch.zeros(2, 8), torch.zeros(2)
+    with pytest.raises(ValueError):
+        tp.tp_token_logprobs(x, None, entropy=one)
+    with pytest.raises(ValueError):
+        tp.tp_policy_loss(x, one.int(), one, one)
+
+
+# ---------------------------------------------------- the oracle's gradients --
+def differences(f, x, h=1e-5):
+    g = np.zeros_like(x)
+    for i in np.ndindex(x.shape):
+        e = np.zeros_like(x)
+        e[i] = h
+        g[i] = (f(x + e).sum() - f(x - e).sum()) / (2 * h)
+    return g
+
+
+# central differences of a smooth loss: h^2 |L'''| / 6 + eps |L| / h, both about 1e-10 here
+@pytest.mark.parametrize("temperature", [1.0, 0.7, 2.0])
+def test_oracle_gradients_against_differences(temperature):
+    rng = np.random.default_rng(3)
+    n, v = 6, 9
+    x, tok = rng.normal(size=(n, v)) * 2, rng.integers(0, v, n)
+    tok[2] = -1
+    adv, w = rng.normal(size=n), rng.random(n) + 0.5
+    gl, gh = rng.normal(size=n), rng.normal(size=n)
+    s = L.token_logprobs(x, tok, temperature)
+    f = lambda y: (lambda r: gl * r["logp"] + gh * r["entropy"])(L.token_logprobs(y, tok, temperature))  # noqa: E731
+    got = L.token_logprobs_backward(x, tok, s["lse"], s["entropy"], gl, gh, temperature)
+    assert np.abs(got - differences(f, x)).max() < 1e-8
+    for old in (None, s["logp"] + rng.normal(size=n) * 0.3):
+        kw = dict(old_logp=old, weight=w, clip_low=0.2, clip_high=0.28, entropy_coef=0.1, temperature=temperature)
+        if old is None:  # on-policy the ratio is 1 and its gradient that of logp: the old log probabilities are this point's
+            kw2 = dict(kw, old_logp=s["logp"])
+        else:
+            kw2 = kw
+        got = L.policy_loss(x, tok, adv, **kw)["dlogits"]
+        assert np.abs(got - differences(lambda y: L.policy_loss(y, tok, adv, **kw2)["loss"], x)).max() < 1e-8
+    ids = np.stack([rng.permutation(v)[:4] for _ in range(n)])
+    ids[1, 2:] = -1
+    ids[3] = -1
+    ids[4, 1] = ids[4, 0]
+    t = rng.normal(size=(n, 4))
+    got = L.distill_loss(x, ids, t, w, temperature)
+    assert np.abs(got["dlogits"] - differences(lambda y: L.distill_loss(y, ids, t, w, temperature)["loss"], x)).max() < 1e-8
+    assert (got["loss"] > -1e-12).all() or ids[4, 0] == ids[4, 1]
+
+
+def test_oracle_by_hand():
+    x = np.log(np.array([[1.0, 2.0, 5.0]]))
+    r = L.token_logprobs(x, np.array([1]), k=2)
+    assert np.allclose([r["logp"][0], r["lse"][0]], [np.log(0.25), np.log(8.0)])
+    assert r["top_ids"].tolist() == [[2, 1]] and np.allclose(r["top_logp"], np.log([[5 / 8, 2 / 8]]))
+    # ratio 2 with A > 0 is clipped at 1.2: no gradient
+    r = L.policy_loss(x, np.array([1]), [3.0], old_logp=[np.log(0.125)])
+    assert np.isclose(r["loss"][0], -3.6) and not r["dlogits"].any()
+    # a teacher that agrees on its two tokens still pulls mass from the third
+    r = L.distill_loss(x, np.array([[2, 1]]), np.log([[5.0, 2.0]]))
+    assert np.isclose(r["loss"][0], np.log(8 / 7)) and np.allclose(r["dlogits"][0], [1 / 8, 2 / 8 - 2 / 7, 5 / 8 - 5 / 7])
