@@ -567,7 +567,7 @@ tp_status tp_tree_advantage(const int32_t* parent, int32_t n_nodes, const int32_
 #define TP_BF16 0
 #define TP_F16 1
 #define TP_F32 2
-#define TP_MAX_VOCAB 393216
+#define TP_MAX_VOCAB 327680
 #define TP_MAX_ALTERNATIVES 128
 #define TP_MAX_TEACHER_LOGITS 512
 

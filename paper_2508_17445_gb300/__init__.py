@@ -53,7 +53,7 @@ TP_SEG_EOS, TP_SEG_BOXED, TP_SEG_FAILED, TP_SEG_MAX_DEPTH = 1, 2, 4, 8
 EVENT_NAMES = {1: "root", 2: "fork", 3: "segment", 4: "output", 5: "prune", 6: "fallback", 7: "done"}
 
 TP_BF16, TP_F16, TP_F32 = 0, 1, 2
-TP_MAX_VOCAB = 393216
+TP_MAX_VOCAB = 327680
 TP_MAX_ALTERNATIVES = 128
 TP_MAX_TEACHER_LOGITS = 512
 

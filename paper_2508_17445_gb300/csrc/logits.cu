@@ -6,24 +6,143 @@
 //   H = ln 2 (log2 s - t / s).
 // The difference is taken before the product: a row of the type's lowest values
 // would overflow in c x_j, and the row's largest terms lose nothing.
+//
+// All of it is bound by HBM: 8 to 20 operations an element against its 2 or 4
+// bytes, so a row is read once. wide_kernel is persistent: a cluster of CTAs takes
+// row after row, each CTA a slice of it, which bulk copies bring into a ring of
+// chunks in shared memory. Sixteen warps take the slice's statistics, send them to
+// every CTA of the cluster through distributed shared memory and, while these
+// travel, begin the next row; then they make the gradient (or find the
+// alternatives) from the same chunks and give them back to the ring. Nothing
+// waits for a whole CTA. backward_kernel needs no statistics and streams.
+//
+// Rows start at any element: 16-byte vectors are counted from the line that the
+// row's logits begin in, and the two vectors at the ends that a row shares with
+// its neighbours are read and written by element, with -inf (p = 0) in the places
+// of the others. A gradient that lies differently in its lines than the logits is
+// shifted into place between neighbouring lanes.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+
+#include <algorithm>
 
 #include "logits.h"
 
 namespace tp {
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kMaxCluster = 8;
+constexpr int kWarps = 8;            // that work on a row's elements
+constexpr int kCopyWarp = kWarps;    // issues the bulk copies
+constexpr int kHelpers = 4;          // warps that look ahead at the rows' own values
+constexpr int kThreads = (kWarps + 1 + kHelpers) * 32;
+constexpr int kRowThreads = kWarps * 32;
+constexpr int kSlots = 4;            // rows whose values and statistics are held at once
+constexpr int kMaxChunks = 32;       // of the ring
+constexpr uint64_t kWaitLimitNs = 2000000000ull;  // bounded waits: 2 s
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNegInf = -INFINITY;
 
+// ------------------------------------------------------------------ pieces --
 __device__ __forceinline__ float exp2_approx(float x) {  // 2 ulp; exp2(-inf) = +0
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+
+// Two fp32 values in one register pair, for the packed add, multiply and fma.
+struct F2 {
+    uint64_t v;
+    F2() = default;
+    __device__ __forceinline__ F2(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+    __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+    __device__ __forceinline__ float sum() const {
+        float a, b;
+        get(a, b);
+        return a + b;
+    }
+};
+__device__ __forceinline__ F2 operator+(F2 a, F2 b) {
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 operator*(F2 a, F2 b) {
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// The address in CTA `rank` of the cluster of what is at `addr` here.
+__device__ __forceinline__ uint32_t map_to(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+// Stores to another CTA's memory that count towards the bytes its barrier `bar` waits for.
+__device__ __forceinline__ void send(uint32_t addr, uint32_t bar, float a, float b, float c, float d) {
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(addr),
+                 "f"(a), "f"(b), "f"(c), "f"(d), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void send(uint32_t addr, uint32_t bar, unsigned long long v) {
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.u64 [%0], %1, [%2];" ::"r"(addr), "l"(v), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {  // arrives too
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ uint64_t global_ns() {
+    uint64_t t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+    return t;
+}
+// Waits for a barrier's phase. A wait that runs out marks the CTA's *dead, and no
+// later one waits again: the kernel ends, and its results are NaN.
+__device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
+    if (mbar_try(bar, parity)) return;
+    const uint64_t t0 = global_ns();
+    for (uint32_t i = 1; !*dead; ++i) {
+        if (mbar_try(bar, parity)) return;
+        if ((i & 63) == 0 && global_ns() - t0 > kWaitLimitNs) *dead = 1;
+    }
+}
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+                 "r"(bytes), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void row_threads_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kRowThreads) : "memory"); }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -37,42 +156,220 @@ __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { retu
 template <>
 __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
 
-__device__ __forceinline__ float load_value(const void* p, int64_t i, int dtype) {
-    if (dtype == TP_F32) return ((const float*)p)[i];
-    if (dtype == TP_F16) return __half2float(((const __half*)p)[i]);
-    return __bfloat162float(((const __nv_bfloat16*)p)[i]);
+// A 16-byte vector of E elements.
+template <typename T>
+struct Vec;
+template <>
+struct Vec<float> {
+    static constexpr uint32_t kNone = 0xff800000u;  // -inf
+    static constexpr int E = 4;
+    static __device__ __forceinline__ void unpack(const uint4& r, float* v) {
+        v[0] = __uint_as_float(r.x), v[1] = __uint_as_float(r.y), v[2] = __uint_as_float(r.z), v[3] = __uint_as_float(r.w);
+    }
+    static __device__ __forceinline__ uint4 pack(const float* v) {
+        return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    }
+    static __device__ __forceinline__ float max_of(const uint4& r) {  // NaN left out
+        return fmaxf(fmaxf(__uint_as_float(r.x), __uint_as_float(r.y)), fmaxf(__uint_as_float(r.z), __uint_as_float(r.w)));
+    }
+};
+template <>
+struct Vec<__nv_bfloat16> {
+    static constexpr uint32_t kNone = 0xff80ff80u;  // -inf
+    static constexpr int E = 8;
+    static __device__ __forceinline__ void unpack(const uint4& r, float* v) {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            v[2 * k] = __uint_as_float(w[k] << 16);
+            v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+        }
+    }
+    static __device__ __forceinline__ uint4 pack(const float* v) {
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+            w[k] = *(const uint32_t*)&h;
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    static __device__ __forceinline__ float max_of(const uint4& r) {
+        const __nv_bfloat162 *a = (const __nv_bfloat162*)&r.x, *b = (const __nv_bfloat162*)&r.y,
+                             *c = (const __nv_bfloat162*)&r.z, *d = (const __nv_bfloat162*)&r.w;
+        const float2 f = __bfloat1622float2(__hmax2(__hmax2(*a, *b), __hmax2(*c, *d)));
+        return fmaxf(f.x, f.y);
+    }
+};
+template <>
+struct Vec<__half> {
+    static constexpr uint32_t kNone = 0xfc00fc00u;  // -inf
+    static constexpr int E = 8;
+    static __device__ __forceinline__ void unpack(const uint4& r, float* v) {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 f = __half22float2(*(const __half2*)&w[k]);
+            v[2 * k] = f.x;
+            v[2 * k + 1] = f.y;
+        }
+    }
+    static __device__ __forceinline__ uint4 pack(const float* v) {
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const __half2 h = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
+            w[k] = *(const uint32_t*)&h;
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    static __device__ __forceinline__ float max_of(const uint4& r) {
+        const __half2 *a = (const __half2*)&r.x, *b = (const __half2*)&r.y, *c = (const __half2*)&r.z, *d = (const __half2*)&r.w;
+        const float2 f = __half22float2(__hmax2(__hmax2(*a, *b), __hmax2(*c, *d)));
+        return fmaxf(f.x, f.y);
+    }
+};
+
+// One row's logits and gradient as vectors: element e of vector v is logit v E + e - lead.
+template <typename T>
+struct Row {
+    static constexpr int E = Vec<T>::E;
+    const T* x;
+    T* dx;
+    int lead, vocab, n_vec;
+    int whole_lo, whole_n;  // vectors whole_lo .. whole_lo + whole_n - 1 hold E elements of the row
+    int shift;              // bytes by which the gradient's vectors begin after a line
+
+    __device__ __forceinline__ Row(const RowArgs& a, int64_t i) {
+        x = (const T*)a.x + i * a.x_stride;
+        dx = a.dx ? (T*)a.dx + i * a.dx_stride : nullptr;
+        lead = (int)((uintptr_t)x & 15) / (int)sizeof(T);
+        vocab = a.vocab;
+        n_vec = (lead + vocab + E - 1) / E;
+        whole_lo = lead > 0;
+        whole_n = max(0, (lead + vocab) / E - whole_lo);
+        shift = (int)(((uintptr_t)dx - (uintptr_t)x) & 15);
+    }
+    __device__ __forceinline__ bool whole(int v) const { return (unsigned)(v - whole_lo) < (unsigned)whole_n; }
+    __device__ __forceinline__ uint4 load_part(int v) const {  // of a vector that is not whole
+        const int j0 = v * E - lead;
+        float f[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) f[e] = j0 + e >= 0 && j0 + e < vocab ? to_f32(x[j0 + e]) : kNegInf;
+        return Vec<T>::pack(f);  // (exact: the values come from T)
+    }
+    __device__ __forceinline__ uint4 load(int v) const {
+        return whole(v) ? __ldcs((const uint4*)(x + (v * E - lead))) : load_part(v);
+    }
+    // Elements e0 .. e1 - 1 of vector v, by element.
+    __device__ __forceinline__ void store_part(int v, const float* f, int e0, int e1) const {
+        const int j0 = v * E - lead;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (e >= e0 && e < e1 && j0 + e >= 0 && j0 + e < vocab) dx[j0 + e] = from_f32<T>(f[e]);
+    }
+    // All lanes of a warp, which hold neighbouring vectors; act: this lane's is one of the row's.
+    __device__ __forceinline__ void store(int v, const float* f, bool act) const {
+        if (shift == 0) {
+            if (act && whole(v))
+                *(uint4*)(dx + (v * E - lead)) = Vec<T>::pack(f);
+            else if (act)
+                store_part(v, f, 0, E);
+            return;
+        }
+        // the line that holds the last elements of the lane before and the first of this one
+        const uint4 own = Vec<T>::pack(f);
+        uint32_t w[8] = {__shfl_up_sync(0xffffffffu, own.x, 1), __shfl_up_sync(0xffffffffu, own.y, 1),
+                         __shfl_up_sync(0xffffffffu, own.z, 1), __shfl_up_sync(0xffffffffu, own.w, 1),
+                         own.x, own.y, own.z, own.w};
+        const int lane = threadIdx.x & 31, back = 16 - shift;
+        const bool line = lane > 0 && act && whole(v) && whole(v - 1);
+        const uint32_t lines = __ballot_sync(0xffffffffu, line);
+        const int split = back / (int)sizeof(T);  // elements of a vector that lie in its first line
+        if (line) {
+            if (back & 4)
+#pragma unroll
+                for (int k = 0; k < 7; ++k) w[k] = w[k + 1];
+            if (back & 8)
+#pragma unroll
+                for (int k = 0; k < 5; ++k) w[k] = w[k + 2];
+            if (back & 2)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], 16);
+            *(uint4*)((char*)(dx + (v * E - lead)) - shift) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else if (act) {
+            store_part(v, f, 0, split);
+        }
+        if (act && (lane == 31 || !(lines >> (lane + 1) & 1))) store_part(v, f, split, E);
+    }
+};
+
+__device__ __forceinline__ float warp_max(float v) {  // NaN left out
+    float m;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(v));
+    return m;
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int off = 16; off; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+    return v;
 }
 
-// Running statistics of a part of a row. m = -inf (and s = t = 0) while it
-// holds no logit above -inf; a NaN or +inf makes s NaN.
+// Statistics of a part of a row. m = -inf (and s = t = 0) while it holds no logit
+// above -inf; a NaN or +inf makes s NaN.
 struct Stats {
     float m = kNegInf, s = 0.f, t = 0.f;
 
-    __device__ __forceinline__ void raise(float m2, float c) {  // m2 >= m
-        const float d = m == kNegInf ? 0.f : c * (m - m2), f = m == kNegInf ? 0.f : exp2_approx(d);
-        t = f * (t + s * fmaxf(d, -1e30f));
-        s *= f;
+    // All lanes: every lane gets the warp's.
+    template <bool ENT>
+    __device__ __forceinline__ void join_warp(float c) {
+        const float most = warp_max(m);
+        const float d = m == kNegInf ? 0.f : c * (m - most), f = m == kNegInf ? 0.f : exp2_approx(d);
+        if (ENT) t = warp_sum(f * (t + s * fmaxf(d, -1e30f)));
+        s = warp_sum(f * s);
+        m = most;
+    }
+};
+
+// A thread's, as it goes; even and odd elements apart.
+struct Running {
+    float m = kNegInf;
+    F2 base{0.f, 0.f};  // -m, or 0 while there is none
+    F2 s{0.f, 0.f}, t{0.f, 0.f};
+
+    __device__ __forceinline__ void raise(float m2, float c) {  // m2 > m
+        const float d = m == kNegInf ? 0.f : fmaxf(c * (m - m2), -1e30f), f = m == kNegInf ? 0.f : exp2_approx(d);
+        const F2 d2(d, d), f2(f, f);
+        t = f2 * fma2(s, d2, t);
+        s = f2 * s;
         m = m2;
+        base = F2(-m2, -m2);
     }
-    __device__ __forceinline__ void add(float x, float c) {
-        if (x > m) raise(x, c);
-        const float d = c * (x - (m == kNegInf ? 0.f : m)), e = exp2_approx(d);
-        s += e;
-        t = fmaf(e, fmaxf(d, -1e30f), t);  // (0 times -inf stays 0)
+    template <typename T, bool ENT, int N>
+    __device__ __forceinline__ void add(const uint4* r, float c) {
+        float m2 = Vec<T>::max_of(r[0]);
+#pragma unroll
+        for (int u = 1; u < N; ++u) m2 = fmaxf(m2, Vec<T>::max_of(r[u]));
+        if (m2 > m) raise(m2, c);
+        const F2 c2(c, c);
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            float x[Vec<T>::E];
+            Vec<T>::unpack(r[u], x);
+#pragma unroll
+            for (int e = 0; e < Vec<T>::E; e += 2) {
+                float d0, d1;
+                ((F2(x[e], x[e + 1]) + base) * c2).get(d0, d1);
+                const F2 p(exp2_approx(d0), exp2_approx(d1));
+                s = s + p;
+                if (ENT) t = fma2(p, F2(fmaxf(d0, -1e30f), fmaxf(d1, -1e30f)), t);  // (0 times -inf stays 0)
+            }
+        }
     }
-    __device__ __forceinline__ void join(Stats b, float c) {
-        if (b.m > m) {
-            const Stats x = *this;
-            *this = b;
-            b = x;
-        }
-        if (b.m == kNegInf) {  // nothing in b, or only NaN
-            s += b.s;
-            return;
-        }
-        b.raise(m, c);
-        s += b.s;
-        t += b.t;
+    __device__ __forceinline__ Stats stats() const {
+        Stats r;
+        r.m = m, r.s = s.sum(), r.t = t.sum();
+        return r;
     }
 };
 
@@ -86,6 +383,7 @@ struct RowResult {
         log2_s = log2f(a.s);
         entropy = empty ? 0.f : kLn2 * (log2_s - a.t / a.s);
         lse = fmaf(log2_s, kLn2, m * inv_t);
+        if (empty) log2_s = 0.f;  // (2^(-inf - 0) = 0)
     }
     // ln p of logit x (-inf of an empty row); not by way of log2 p, which overflows for the type's lowest values
     __device__ __forceinline__ float logp(float x) const { return empty ? kNegInf : fmaf(inv_t, x - m, -kLn2 * log2_s); }
@@ -101,184 +399,860 @@ __device__ __forceinline__ float policy_term(float logp, float a, const float* o
     return a == 0.f ? 0.f : -fminf(r * a, fminf(fmaxf(r, 1.f - lo), 1.f + hi) * a);
 }
 
-template <typename V, typename Op>
-__device__ __forceinline__ V block_reduce(V v, Op op, V* smem) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (int off = 16; off; off >>= 1) {
-        V o;
-        static_assert(sizeof(V) % 4 == 0);
-        uint32_t* d = (uint32_t*)&o;
-        const uint32_t* w = (const uint32_t*)&v;
-        for (int k = 0; k < (int)sizeof(V) / 4; ++k) d[k] = __shfl_xor_sync(0xffffffffu, w[k], off);
-        v = op(v, o);
-    }
-    __syncthreads();
-    if (lane == 0) smem[warp] = v;
-    __syncthreads();
-    v = smem[0];
-    for (int k = 1; k < kThreads / 32; ++k) v = op(v, smem[k]);
-    return v;
+__device__ __forceinline__ float load_value(const void* p, int64_t i, int dtype) {
+    if (dtype == TP_F32) return ((const float*)p)[i];
+    if (dtype == TP_F16) return __half2float(((const __half*)p)[i]);
+    return __bfloat162float(((const __nv_bfloat16*)p)[i]);
 }
 
-__device__ __forceinline__ uint32_t order_key(float x) {  // ascending with x; -0 as +0
-    const uint32_t b = __float_as_uint(x + 0.f);
-    return b & 0x80000000u ? ~b : b | 0x80000000u;
+// ------------------------------------------------------------ alternatives --
+// The k largest logits of a row, of equal ones the lower id first. A key holds
+// both: the logit in an order of unsigned integers above the complement of its id.
+// Each CTA keeps the k largest keys of its slice, the first CTA merges them.
+//
+// A thread's maximum is known from the statistics. Where each of a CTA's W warps
+// has ceil(k / W) lanes whose maximum is at least b, the CTA has k logits that are,
+// so nothing below the largest b of the cluster's CTAs is among the row's k. What
+// is not below it is a short list in all but contrived rows (few distinct values,
+// all large logits in one thread's places); where it is longer than kList, the
+// CTA finds its k-th largest key exactly, by digits.
+constexpr int kList = 256;
+
+typedef unsigned long long Key;
+
+__device__ __forceinline__ Key make_key(float x, int id) {
+    const uint32_t b = __float_as_uint(x + 0.f);  // -0 as +0
+    return (Key)(b & 0x80000000u ? ~b : b | 0x80000000u) << 32 | (0xffffffffu - (uint32_t)id);
+}
+__device__ __forceinline__ int key_id(Key k) { return (int)(0xffffffffu - (uint32_t)k); }
+__device__ __forceinline__ float key_value(Key k) {
+    const uint32_t u = (uint32_t)(k >> 32);
+    return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
 }
 
-enum { OP_LOGPROBS, OP_BACKWARD, OP_POLICY, OP_DISTILL };
+struct TopShared {
+    Key list[kList];
+    Key best[2][kMaxCluster][TP_MAX_ALTERNATIVES];  // where this CTA merges: each CTA's keys, descending, 0 where none is left
+    uint64_t full[2];                               // best's barriers
+    int n, digit, rest;
+    int hist[256];
+};
 
-// The plainest form: one CTA a row, every pass read from memory.
-template <typename T, int OP>
-__global__ void __launch_bounds__(kThreads) row_kernel(const RowArgs a) {
-    __shared__ Stats sh_stats[kThreads / 32];
-    __shared__ unsigned long long sh_key[kThreads / 32];
-    __shared__ float sh_f[kThreads / 32];
-    const int64_t i = blockIdx.x;
-    const int V = a.vocab, tid = threadIdx.x;
-    const T* x = (const T*)a.x + i * a.x_stride;
-    T* dx = (T*)a.dx + i * a.dx_stride;
-    const float c = kLog2e / a.temperature, inv_t = 1.f / a.temperature;
-    const int32_t tok = OP != OP_DISTILL && a.tokens ? a.tokens[i] : 0;
-    bool live = tok >= 0;
-    float q_max = kNegInf, q_sum = 0.f;
-    bool q_bad = false;
-    if (OP == OP_DISTILL) {
-        for (int k = tid; k < a.k; k += kThreads)
-            if (a.teacher_ids[i * a.k + k] >= 0) {
-                const float v = load_value(a.teacher_logits, i * a.k + k, a.teacher_dtype);
-                q_bad |= isnan(v) || v == INFINITY;
-                q_max = fmaxf(q_max, v);
+// One row's chunks in the ring, as the working warps see them: groups of 32
+// vectors, group g of a chunk is warp (g % kWarps)'s.
+template <int N>
+struct Count {
+    static constexpr int n = N;
+};
+template <typename T>
+struct Slice {
+    static constexpr int E = Vec<T>::E;
+    const uint8_t* ring;
+    int slot, slots, slot_bytes;  // the first chunk's
+    int first, n, chunk;          // the slice's first vector, its vectors, a chunk's
+
+    // f(Count<M>, vectors read (M, kRowThreads apart), the first's number in the row, act), M = N or 1;
+    // wait(slot) before a chunk, done(slot) after it.
+    template <int N, typename W, typename F, typename D>
+    __device__ __forceinline__ void each(W wait, F f, D done) const {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        int at = slot;
+        for (int v0 = 0; v0 < n; v0 += chunk) {
+            wait(at);
+            const uint4* data = (const uint4*)(ring + (size_t)at * slot_bytes) + lane;
+            const int m = min(chunk, n - v0), v = first + v0 + lane;
+            int g = warp * 32;
+            for (; g + (N - 1) * kRowThreads + 32 <= m; g += N * kRowThreads) {
+                uint4 r[N];
+#pragma unroll
+                for (int u = 0; u < N; ++u) r[u] = data[g + u * kRowThreads];
+                f(Count<N>{}, r, v + g, true);
             }
-        q_max = block_reduce(q_max, [](float p, float q) { return fmaxf(p, q); }, sh_f);
-        q_bad = __syncthreads_or(q_bad);
-        live = q_bad || q_max > kNegInf;
-        if (live && !q_bad) {
-            for (int k = tid; k < a.k; k += kThreads)
-                if (a.teacher_ids[i * a.k + k] >= 0)
-                    q_sum += exp2_approx(c * (load_value(a.teacher_logits, i * a.k + k, a.teacher_dtype) - q_max));
-            q_sum = block_reduce(q_sum, [](float p, float q) { return p + q; }, sh_f);
-        }
-    }
-    if (!live) {
-        if (a.dx)
-            for (int j = tid; j < V; j += kThreads) dx[j] = from_f32<T>(0.f);
-        if (tid == 0) {
-            if (a.logp) a.logp[i] = 0.f;
-            if (a.entropy) a.entropy[i] = 0.f;
-            if (a.lse) a.lse[i] = 0.f;
-            if (a.loss) a.loss[i] = 0.f;
-        }
-        if (OP == OP_LOGPROBS)
-            for (int k = tid; k < a.k; k += kThreads) {
-                a.top_ids[i * a.k + k] = -1;
-                a.top_logp[i * a.k + k] = kNegInf;
+            for (; g < m; g += kRowThreads) {
+                uint4 r = make_uint4(Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone);
+                const bool act = g + lane < m;
+                if (act) r = data[g];
+                f(Count<1>{}, &r, v + g, act);
             }
-        return;
-    }
-    float x_tok = NAN;
-    if (OP != OP_DISTILL && a.tokens && tok < V) x_tok = to_f32(x[tok]);
-    if (OP == OP_BACKWARD) {
-        const float lse = a.lse_in[i], gl = a.dlogp ? a.dlogp[i] : 0.f, gh = a.dentropy ? a.dentropy[i] : 0.f;
-        const float h = a.dentropy ? a.entropy_in[i] : 0.f;
-        const bool bad = a.dlogp && tok >= V;
-        for (int j = tid; j < V; j += kThreads) {
-            const float lp = to_f32(x[j]) * inv_t - lse, p = exp2_approx(lp * kLog2e);
-            float d = gl * ((a.dlogp && j == tok ? 1.f : 0.f) - p) - gh * p * (fmaxf(lp, -1e30f) + h);
-            if (lse == kNegInf) d = 0.f;
-            if (bad) d = NAN;
-            dx[j] = from_f32<T>(d * inv_t);
+            done(at);
+            if (++at == slots) at = 0;
         }
-        return;
     }
-    Stats st;
-    for (int j = tid; j < V; j += kThreads) st.add(to_f32(x[j]), c);
-    st = block_reduce(st, [c](Stats p, Stats q) { p.join(q, c); return p; }, sh_stats);
-    const RowResult r(st, c, inv_t);
-    if (OP == OP_LOGPROBS) {
-        if (tid == 0) {
-            if (a.logp) a.logp[i] = tok < V ? r.logp(x_tok) : NAN;
-            if (a.entropy) a.entropy[i] = r.entropy;
-            if (a.lse) a.lse[i] = r.lse;
+    // f(logit, id) for every logit above -inf of this thread's vectors.
+    template <typename F>
+    __device__ __forceinline__ void each_logit(const Row<T>& row, F f) const {
+        each<1>([](int) {}, [&](Count<1>, const uint4* r, int v, bool) {
+            float x[E];
+            Vec<T>::unpack(r[0], x);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (x[e] > kNegInf) f(x[e], v * E + e - row.lead);
+        }, [](int) {});
+    }
+};
+
+// The k-th largest key of the slice by its digits of 8 bits, the highest first
+// (0 if there are fewer). The id's highest digit is the same in all.
+template <typename T>
+__device__ Key kth_key(const Slice<T>& slice, const Row<T>& row, int k, TopShared& sh) {
+    Key found = 0, mask = 0;
+    int rest = k;
+    for (int shift = 56; shift >= 0; shift -= 8) {
+        if (shift == 24) {
+            found |= (Key)0xff << 24;
+            mask |= (Key)0xff << 24;
+            continue;
         }
-        unsigned long long last = ~0ull;
-        for (int k = 0; k < a.k; ++k) {
-            unsigned long long best = 0;
-            if (!isnan(r.lse))
-                for (int j = tid; j < V; j += kThreads) {
-                    const float v = to_f32(x[j]);
-                    const unsigned long long key = (unsigned long long)order_key(v) << 32 | (0xffffffffu - j);
-                    if (v > kNegInf && key < last && key > best) best = key;
+        for (int b = threadIdx.x; b < 256; b += kRowThreads) sh.hist[b] = 0;
+        row_threads_sync();
+        slice.each_logit(row, [&](float x, int id) {
+            const Key key = make_key(x, id);
+            if ((key & mask) == found) atomicAdd(&sh.hist[(int)(key >> shift) & 255], 1);
+        });
+        row_threads_sync();
+        if (threadIdx.x < 32) {  // lane l: digits 255 - 8 l downwards
+            int own[8], sum = 0;
+            for (int b = 0; b < 8; ++b) sum += own[b] = sh.hist[255 - 8 * threadIdx.x - b];
+            int before = sum;
+            for (int off = 1; off < 32; off <<= 1) {
+                const int o = __shfl_up_sync(0xffffffffu, before, off);
+                if ((int)threadIdx.x >= off) before += o;
+            }
+            if (threadIdx.x == 31) sh.digit = before < rest ? -1 : 0;
+            __syncwarp();
+            before -= sum;
+            if (before < rest && before + sum >= rest) {
+                int b = 0;
+                while (before + own[b] < rest) before += own[b++];
+                sh.digit = 255 - 8 * threadIdx.x - b;
+                sh.rest = rest - before;
+            }
+        }
+        row_threads_sync();
+        if (sh.digit < 0) return 0;
+        found |= (Key)sh.digit << shift;
+        mask |= (Key)0xff << shift;
+        rest = sh.rest;
+    }
+    return found;
+}
+
+// This CTA's k largest keys, descending, sent to the CTA `to` of the cluster; the
+// working warps. own_max: the thread's largest logit; bound: see above.
+template <typename T>
+__device__ void send_best(const Slice<T>& slice, const Row<T>& row, int k, float own_max, float bound, TopShared& sh, int turn,
+                          uint32_t rank, uint32_t to) {
+    if (threadIdx.x == 0) sh.n = 0;
+    row_threads_sync();
+    if (__any_sync(0xffffffffu, own_max >= bound))
+        slice.each_logit(row, [&](float x, int id) {
+            if (x >= bound) {
+                const int at = atomicAdd(&sh.n, 1);
+                if (at < kList) sh.list[at] = make_key(x, id);
+            }
+        });
+    row_threads_sync();
+    if (sh.n > kList) {
+        const Key kth = kth_key(slice, row, k, sh);
+        if (threadIdx.x == 0) sh.n = 0;
+        row_threads_sync();
+        slice.each_logit(row, [&](float x, int id) {
+            const Key key = make_key(x, id);
+            if (key >= kth) {
+                const int at = atomicAdd(&sh.n, 1);
+                if (at < kList) sh.list[at] = key;  // (k of them)
+            }
+        });
+        row_threads_sync();
+    }
+    const int m = min(sh.n, kList);
+    const uint32_t dst = map_to(smem_addr(&sh.best[turn][rank][0]), to), bar = map_to(smem_addr(&sh.full[turn]), to);
+    for (int p = threadIdx.x; p < max(m, k); p += kRowThreads) {
+        if (p >= m) {
+            send(dst + p * 8, bar, 0ull);
+            continue;
+        }
+        const Key key = sh.list[p];
+        int place = 0;
+        for (int q = 0; q < m; ++q) place += sh.list[q] > key;
+        if (place < k) send(dst + place * 8, bar, key);
+    }
+    row_threads_sync();  // the list is free again
+}
+
+// The row's k largest keys, from every CTA's; the working warps.
+__device__ void merge_best(const RowArgs& a, int64_t i, int cta_n, const RowResult& r, const TopShared& sh, int turn) {
+    const int k = a.k;
+    const bool nan = isnan(r.lse);
+    for (int p = threadIdx.x; p < cta_n * k; p += kRowThreads) {
+        const int own = p / k, at = p - own * k;
+        const Key key = sh.best[turn][own][at];
+        int place = at;
+        for (int q = 0; q < cta_n && place < k; ++q) {
+            if (q == own) continue;
+            int lo = 0, hi = k;  // how many of q's come before: larger, or for "none" (0) the lower CTA's
+            while (lo < hi) {
+                const int mid = (lo + hi) / 2;
+                const Key o = sh.best[turn][q][mid];
+                if (o > key || (o == key && q < own))
+                    lo = mid + 1;
+                else
+                    hi = mid;
+            }
+            place += lo;
+        }
+        if (place < k) {
+            const bool some = key != 0 && !nan;
+            a.top_ids[i * k + place] = some ? key_id(key) : -1;
+            a.top_logp[i * k + place] = nan ? NAN : some ? r.logp(key_value(key)) : kNegInf;
+        }
+    }
+}
+
+// --------------------------------------------------------------- the rows --
+enum { OP_LOGPROBS, OP_POLICY, OP_DISTILL };
+
+// A row's own values, looked up ahead of its turn.
+struct RowInfo {
+    int32_t live, tok;  // not live: padding
+    float x_tok, w, adv, old;
+    int32_t bad, n_own; // distillation: the teacher's answer is not one; its tokens in this CTA's slice
+    int32_t repeats;    // some of these may come twice
+    uint4 edge[2];      // the slice's vectors that the row shares with its neighbours, the first and the last
+};
+
+struct TeacherList {
+    int32_t id[TP_MAX_TEACHER_LOGITS];   // -1: no share
+    float q[TP_MAX_TEACHER_LOGITS];
+    float x[TP_MAX_TEACHER_LOGITS];      // the student's logits (the first CTA's, and of the slice's tokens)
+    int16_t own[TP_MAX_TEACHER_LOGITS];  // places of the slice's tokens
+};
+constexpr int kSeenWords = 256;
+struct TeacherShared {
+    TeacherList list[kSlots];
+    uint32_t seen[kHelpers][kSeenWords];  // a bit for the tokens of equal residue
+};
+struct NoShared {};
+
+template <int OP, bool RES>
+struct OpShared {
+    typedef NoShared type;
+};
+template <>
+struct OpShared<OP_LOGPROBS, true> {
+    typedef TopShared type;
+};
+template <bool RES>
+struct OpShared<OP_DISTILL, RES> {
+    typedef TeacherShared type;
+};
+
+struct RowShared {
+    float4 parts[kSlots][kMaxCluster][kWarps];  // statistics (m, s, t) and bound of every warp of the cluster
+    RowInfo info[kSlots];
+    uint64_t full[kMaxChunks], empty[kMaxChunks];
+    uint64_t info_full[kSlots], info_empty[kSlots], parts_full[kSlots];
+    int dead;
+};
+
+struct Plan {
+    int cta_n;          // CTAs a cluster
+    int chunk, chunks;  // vectors a chunk, chunks of the ring
+    int per_cta;        // vectors a slice
+    int ahead;          // whether a row's statistics are begun before the last row is done
+};
+
+// A lane's share of a row's edges: lanes 0 .. E - 1 the first vector's elements, 16 .. the last one's.
+template <typename T>
+__device__ __forceinline__ T edge_element(const Row<T>& row, int first, int per_cta) {
+    constexpr int E = Vec<T>::E;
+    const int lane = threadIdx.x & 31, e = lane & 15, v = lane < 16 ? 0 : row.n_vec - 1, j = v * E + e - row.lead;
+    if (e >= E || row.whole(v) || v < first || v >= first + per_cta || j < 0 || j >= row.vocab) return from_f32<T>(kNegInf);
+    return row.x[j];
+}
+template <typename T>
+__device__ __forceinline__ void keep_edge(RowInfo& info, T x) {
+    const int lane = threadIdx.x & 31, e = lane & 15;
+    if (e < Vec<T>::E) ((T*)&info.edge[lane / 16])[e] = x;
+}
+
+// A helper warp's look ahead at one row of a distillation: the teacher's shares.
+template <typename T>
+__device__ void teacher_ahead(const RowArgs& a, int64_t i, const Row<T>& row, int first, int n, uint32_t rank, RowInfo& info,
+                              TeacherList& list, uint32_t* seen) {
+    const int lane = threadIdx.x & 31;
+    const float c = kLog2e / a.temperature;
+    const int32_t* ids = a.teacher_ids + i * a.k;
+    float best = kNegInf;
+    bool bad = false;
+    for (int k = lane; k < a.k; k += 32)
+        if (ids[k] >= 0) {
+            const float v = load_value(a.teacher_logits, i * a.k + k, a.teacher_dtype);
+            bad |= isnan(v) || v == INFINITY;
+            best = fmaxf(best, v);
+        }
+    best = warp_max(best);
+    bad = __any_sync(0xffffffffu, bad);
+    const bool live = bad || best > kNegInf;
+    bool off = false, twice = false;
+    int n_own = 0;
+    if (live && !bad) {
+        float sum = 0.f;
+        for (int k = lane; k < a.k; k += 32)
+            if (ids[k] >= 0) sum += exp2_approx(c * (load_value(a.teacher_logits, i * a.k + k, a.teacher_dtype) - best));
+        sum = warp_sum(sum);
+        const int lo = first * Row<T>::E - row.lead, hi = lo + n * Row<T>::E;
+        for (int k0 = 0; k0 < a.k; k0 += 32) {
+            const int k = k0 + lane;
+            int32_t id = -1;
+            float q = 0.f;
+            if (k < a.k) {
+                id = ids[k];
+                if (id >= 0) q = exp2_approx(c * (load_value(a.teacher_logits, i * a.k + k, a.teacher_dtype) - best)) / sum;
+                if (!(q > 0.f)) id = -1;
+                off |= id >= row.vocab;
+                const bool own = id >= 0 && id < row.vocab && id >= lo && id < hi;
+                list.id[k] = id;
+                list.q[k] = q;
+                list.x[k] = own || (rank == 0 && id >= 0 && id < row.vocab) ? to_f32(row.x[id]) : 0.f;
+                if (own) {
+                    const uint32_t bit = id % (32 * kSeenWords);
+                    twice |= atomicOr(&seen[bit / 32], 1u << (bit % 32)) >> (bit % 32) & 1;
                 }
-            best = block_reduce(best, [](unsigned long long p, unsigned long long q) { return p > q ? p : q; }, sh_key);
-            if (tid == 0) {
-                const int32_t id = best ? (int32_t)(0xffffffffu - (uint32_t)best) : -1;
-                a.top_ids[i * a.k + k] = id;
-                a.top_logp[i * a.k + k] = isnan(r.lse) ? NAN : id < 0 ? kNegInf : r.logp(to_f32(x[id]));
+                id = own ? id : -1;
             }
-            last = best;
+            const uint32_t owners = __ballot_sync(0xffffffffu, id >= 0);
+            if (id >= 0) list.own[n_own + __popc(owners & ((1u << lane) - 1))] = (int16_t)k;
+            n_own += __popc(owners);
         }
+        __syncwarp();
+        for (int k = lane; k < n_own; k += 32) seen[list.id[list.own[k]] % (32 * kSeenWords) / 32] = 0;
+        off = __any_sync(0xffffffffu, off);
+        twice = __any_sync(0xffffffffu, twice);
+    }
+    if (lane == 0) {
+        info.live = live;
+        info.bad = bad || off;
+        info.n_own = n_own;
+        info.repeats = twice;
+        info.w = a.weight ? a.weight[i] : 1.f;
+    }
+    __syncwarp();
+}
+
+// RES: the slice stays in the ring until the row's statistics are known, for a
+// gradient or alternatives. ENT: the entropy is asked for (or in the gradient).
+template <typename T, int OP, bool RES, bool ENT>
+__global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant__ RowArgs a, const __grid_constant__ Plan plan) {
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ RowShared sm;
+    __shared__ typename OpShared<OP, RES>::type sh;
+    constexpr bool TOP = OP == OP_LOGPROBS && RES;
+    constexpr int E = Vec<T>::E;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int cta_n = plan.cta_n, slot_bytes = plan.chunk * 16;
+    const uint32_t rank = cluster_rank();
+    const int64_t groups = gridDim.x / cta_n, group = blockIdx.x / cta_n;
+    const int64_t rows = (a.n - group + groups - 1) / groups;  // row q of the cluster is group + q groups
+    const int first = rank * plan.per_cta;
+    const uint32_t full = smem_addr(sm.full), empty = smem_addr(sm.empty);
+    const uint32_t info_full = smem_addr(sm.info_full), info_empty = smem_addr(sm.info_empty);
+    const uint32_t parts_full = smem_addr(sm.parts_full);
+    if (tid == 0) {
+        for (int k = 0; k < plan.chunks; ++k) {
+            mbar_init(full + 8 * k, 1);
+            mbar_init(empty + 8 * k, kWarps);
+        }
+        for (int k = 0; k < kSlots; ++k) {
+            mbar_init(info_full + 8 * k, 1);
+            mbar_init(info_empty + 8 * k, kWarps + 1);
+            mbar_init(parts_full + 8 * k, 1);
+        }
+        if constexpr (TOP)
+            for (int k = 0; k < 2; ++k) mbar_init(smem_addr(&sh.full[k]), 1);
+        sm.dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if constexpr (OP == OP_DISTILL)
+        for (int k = tid; k < kHelpers * kSeenWords; k += kThreads) (&sh.seen[0][0])[k] = 0;
+    __syncthreads();
+    cluster_arrive();  // every CTA's barriers are there
+    cluster_wait();
+
+    if (warp > kCopyWarp) {
+        // ---- looking ahead: helper h at rows h, h + kHelpers, ...
+        const int h = warp - kCopyWarp - 1;
+        static_assert(kHelpers == kSlots);
+        if constexpr (OP == OP_DISTILL) {
+            for (int64_t q = h; q < rows; q += kHelpers) {
+                const int64_t i = group + q * groups;
+                const Row<T> row(a, i);
+                const T edge = edge_element(row, first, plan.per_cta);
+                mbar_wait(info_empty + 8 * h, (q / kSlots & 1) ^ 1, &sm.dead);
+                keep_edge(sm.info[h], edge);
+                teacher_ahead(a, i, row, first, max(0, min(plan.per_cta, row.n_vec - first)), rank, sm.info[h], sh.list[h], sh.seen[h]);
+                if (lane == 0) mbar_arrive(info_full + 8 * h);
+            }
+        } else {
+            int32_t tok = 0;
+            float x_tok = NAN, w = 1.f, adv = 0.f, old = 0.f;
+            T edge = from_f32<T>(kNegInf);
+            auto look = [&](int64_t q) {  // (a gradient in place comes later: it waits for this row's copy, which waits for this)
+                if (q >= rows) return;
+                const int64_t i = group + q * groups;
+                const Row<T> row(a, i);
+                tok = a.tokens ? a.tokens[i] : 0;
+                if (lane == 0) {
+                    w = a.weight ? a.weight[i] : 1.f;
+                    if (OP == OP_POLICY) {
+                        adv = a.advantage[i];
+                        old = a.old_logp ? a.old_logp[i] : 0.f;
+                    }
+                }
+                x_tok = NAN;
+                if (tok >= 0) {
+                    edge = edge_element(row, first, plan.per_cta);
+                    if (lane == 0 && a.tokens && tok < row.vocab) x_tok = to_f32(row.x[tok]);
+                }
+            };
+            look(h);
+            for (int64_t q = h; q < rows; q += kHelpers) {
+                mbar_wait(info_empty + 8 * h, (q / kSlots & 1) ^ 1, &sm.dead);
+                RowInfo& info = sm.info[h];
+                keep_edge(info, edge);
+                if (lane == 0) {
+                    info.tok = tok;
+                    info.live = tok >= 0;
+                    info.x_tok = x_tok;
+                    info.w = w;
+                    info.adv = adv;
+                    info.old = old;
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(info_full + 8 * h);
+                look(q + kHelpers);
+            }
+        }
+    } else if (warp == kCopyWarp) {
+        // ---- the copies
+        if (lane == 0) {
+            int slot = 0, phase = 0;
+            for (int64_t q = 0; q < rows; ++q) {
+                const int s = q % kSlots;
+                mbar_wait(info_full + 8 * s, q / kSlots & 1, &sm.dead);
+                const bool live = sm.info[s].live;
+                const uint4 head = sm.info[s].edge[0], tail = sm.info[s].edge[1];
+                mbar_arrive(info_empty + 8 * s);
+                if (!live) continue;
+                const Row<T> row(a, group + q * groups);
+                const int end = min(first + plan.per_cta, row.n_vec);
+                for (int v = first; v < end; v += plan.chunk) {
+                    mbar_wait(empty + 8 * slot, phase ^ 1, &sm.dead);
+                    const int last = min(v + plan.chunk, end) - 1;
+                    uint4* to = (uint4*)(ring + (size_t)slot * slot_bytes);
+                    if (v == 0 && !row.whole(0)) to[0] = head;
+                    if (last == row.n_vec - 1 && !row.whole(last) && last > 0) to[last - v] = tail;
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before a later copy to the same place
+                    const int v0 = max(v, row.whole_lo), v1 = min(min(v + plan.chunk, end), row.whole_lo + row.whole_n);
+                    if (v1 > v0 && !*(volatile int*)&sm.dead) {
+                        mbar_expect(full + 8 * slot, (v1 - v0) * 16);
+                        bulk_copy(smem_addr(ring) + slot * slot_bytes + (v0 - v) * 16, row.x + ((int64_t)v0 * E - row.lead),
+                                  (v1 - v0) * 16, full + 8 * slot);
+                    } else {
+                        mbar_arrive(full + 8 * slot);
+                    }
+                    if (++slot == plan.chunks) slot = 0, phase ^= 1;
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---- the rows
+        const float c = kLog2e / a.temperature, inv_t = 1.f / a.temperature;
+        int slot_a = 0, phase_a = 0, slot_b = 0;  // the ring, at the row whose statistics are taken and at the one after
+        int64_t live_a = 0, live_b = 0;  // rows with statistics so far
+        float max_a = kNegInf, max_b = kNegInf;
+        auto slice_at = [&](const Row<T>& row, int slot) {
+            return Slice<T>{ring, slot, plan.chunks, slot_bytes, first, max(0, min(plan.per_cta, row.n_vec - first)), plan.chunk};
+        };
+
+        auto statistics = [&](int64_t q) {
+            const int s = q % kSlots;
+            mbar_wait(info_full + 8 * s, q / kSlots & 1, &sm.dead);
+            if (!sm.info[s].live) return;
+            const Row<T> row(a, group + q * groups);
+            const Slice<T> slice = slice_at(row, slot_a);
+            Running run;
+            slice.template each<4>(
+                [&](int slot) { mbar_wait(full + 8 * slot, phase_a, &sm.dead); },
+                [&](auto count, const uint4* r, int, bool) { run.add<T, ENT, decltype(count)::n>(r, c); },
+                [&](int slot) {
+                    if (!RES) {
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(empty + 8 * slot);
+                    }
+                    if (++slot_a == plan.chunks) slot_a = 0, phase_a ^= 1;
+                });
+            Stats st = run.stats();
+            float bound = kNegInf;
+            max_a = st.m;
+            if constexpr (TOP) {  // this warp's ceil(k / kWarps)-th largest of its lanes' maxima
+                float v = st.m;
+#pragma unroll
+                for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll
+                    for (int step = size >> 1; step; step >>= 1) {
+                        const float o = __shfl_xor_sync(0xffffffffu, v, step);
+                        const bool down = (lane & size) == 0, low = (lane & step) == 0;
+                        v = down == low ? fmaxf(v, o) : fminf(v, o);
+                    }
+                bound = __shfl_sync(0xffffffffu, v, (a.k + kWarps - 1) / kWarps - 1);
+            }
+            st.join_warp<ENT>(c);
+            const int x = live_a++ % kSlots;
+            if (tid == 0) mbar_expect(parts_full + 8 * x, cta_n * kWarps * 16);
+            if (lane < cta_n)
+                send(map_to(smem_addr(&sm.parts[x][rank][warp]), lane), map_to(parts_full + 8 * x, lane), st.m, st.s, st.t, bound);
+        };
+
+        auto rest = [&](int64_t q) {
+            const int s = q % kSlots;
+            const int64_t i = group + q * groups;
+            const RowInfo& info = sm.info[s];
+            const Row<T> row(a, i);
+            const Slice<T> slice = slice_at(row, slot_b);
+            const bool tells = rank == 0 && tid == 0;  // writes the row's own results
+            if (!info.live) {
+                if constexpr (RES && OP != OP_LOGPROBS) {
+                    const float zero[E] = {};
+                    for (int g = warp * 32; g < slice.n; g += kRowThreads) row.store(first + g + lane, zero, g + lane < slice.n);
+                }
+                if (tells) {
+                    if (a.logp) a.logp[i] = 0.f;
+                    if (a.entropy) a.entropy[i] = 0.f;
+                    if (a.lse) a.lse[i] = 0.f;
+                    if (a.loss) a.loss[i] = 0.f;
+                }
+                if (TOP && rank == 0)
+                    for (int k = tid; k < a.k; k += kRowThreads) {
+                        a.top_ids[i * a.k + k] = -1;
+                        a.top_logp[i * a.k + k] = kNegInf;
+                    }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(info_empty + 8 * s);
+                return;
+            }
+            const int x = live_b % kSlots;
+            mbar_wait(parts_full + 8 * x, live_b / kSlots & 1, &sm.dead);
+            // every warp joins all parts, in the same order
+            Stats all;
+            float bound = kNegInf;
+            {
+                constexpr int kMost = (kMaxCluster * kWarps + 31) / 32;
+                float4 p[kMost];
+                const float4* parts = &sm.parts[x][0][0];
+#pragma unroll
+                for (int k = 0; k < kMost; ++k) {
+                    p[k] = make_float4(kNegInf, 0.f, 0.f, INFINITY);
+                    if (lane + 32 * k < cta_n * kWarps) p[k] = parts[lane + 32 * k];
+                    all.m = fmaxf(all.m, p[k].x);
+                }
+                all.m = warp_max(all.m);
+#pragma unroll
+                for (int k = 0; k < kMost; ++k) {
+                    const float d = p[k].x == kNegInf ? 0.f : c * (p[k].x - all.m), f = p[k].x == kNegInf ? 0.f : exp2_approx(d);
+                    if (ENT) all.t += f * (p[k].z + p[k].y * fmaxf(d, -1e30f));
+                    all.s += f * p[k].y;
+                    if constexpr (TOP) {  // the largest over the CTAs of the least over their warps
+                        float least = p[k].w;
+#pragma unroll
+                        for (int off = kWarps / 2; off; off >>= 1) least = fminf(least, __shfl_xor_sync(0xffffffffu, least, off));
+                        if (least < INFINITY) bound = fmaxf(bound, least);
+                    }
+                }
+                all.s = warp_sum(all.s);
+                if (ENT) all.t = warp_sum(all.t);
+                if constexpr (TOP)
+#pragma unroll
+                    for (int off = kWarps; off < 32; off <<= 1) bound = fmaxf(bound, __shfl_xor_sync(0xffffffffu, bound, off));
+            }
+            if (*(volatile int*)&sm.dead) all.s = NAN;
+            const RowResult res(all, c, inv_t);
+            const int32_t tok = info.tok;
+
+            float k0 = 0.f, k1 = 0.f, k2 = 0.f;  // the gradient p (k0 + k1 log2 p) + [j = token] k2
+            if constexpr (OP == OP_LOGPROBS) {
+                if (tells) {
+                    if (a.logp) a.logp[i] = tok < row.vocab ? res.logp(info.x_tok) : NAN;
+                    if (a.entropy) a.entropy[i] = res.entropy;
+                    if (a.lse) a.lse[i] = res.lse;
+                }
+            }
+            if constexpr (OP == OP_POLICY) {
+                float g;
+                const float logp = tok < row.vocab ? res.logp(info.x_tok) : NAN;
+                const float term = policy_term(logp, info.adv, a.old_logp ? &info.old : nullptr, 0, a.clip_low, a.clip_high, g);
+                if (tells) {
+                    a.loss[i] = info.w * (ENT ? term - a.entropy_coef * res.entropy : term);
+                    if (a.logp) a.logp[i] = logp;
+                    if (ENT && a.entropy) a.entropy[i] = res.entropy;
+                }
+                const float wt = info.w * inv_t;
+                k0 = wt * (ENT ? a.entropy_coef * res.entropy - g : -g);
+                k1 = ENT ? wt * a.entropy_coef * kLn2 : 0.f;
+                k2 = res.empty ? 0.f : wt * g;
+            }
+            if constexpr (OP == OP_DISTILL) {
+                k0 = info.bad ? NAN : info.w * inv_t;
+                if (rank == 0 && warp == kWarps - 1) {
+                    const TeacherList& list = sh.list[s];
+                    float part = 0.f;
+                    if (!info.bad)
+                        for (int k = lane; k < a.k; k += 32)
+                            if (list.id[k] >= 0) part += list.q[k] * (logf(list.q[k]) - res.logp(list.x[k]));
+                    part = warp_sum(part);
+                    if (lane == 0) a.loss[i] = info.bad || isnan(res.lse) ? NAN : info.w * part;
+                }
+            }
+            if constexpr (RES && OP != OP_LOGPROBS) {
+                const int tok_vec = OP == OP_POLICY && tok < row.vocab ? (tok + row.lead) / E : -1;
+                const F2 base(-res.m, -res.m), c2(c, c), less(-res.log2_s, -res.log2_s), k02(k0, k0), k12(k1, k1);
+                slice.template each<2>(
+                    [](int) {},
+                    [&](auto count, const uint4* r, int v0, bool act) {
+#pragma unroll
+                        for (int u = 0; u < decltype(count)::n; ++u) {
+                            const int v = v0 + u * kRowThreads;
+                            float y[E];
+                            Vec<T>::unpack(r[u], y);
+#pragma unroll
+                            for (int e = 0; e < E; e += 2) {
+                                float d0, d1;
+                                fma2(F2(y[e], y[e + 1]) + base, c2, less).get(d0, d1);
+                                const F2 p(exp2_approx(d0), exp2_approx(d1));
+                                (p * (ENT ? fma2(k12, F2(fmaxf(d0, -1e30f), fmaxf(d1, -1e30f)), k02) : k02)).get(y[e], y[e + 1]);
+                            }
+                            if (OP == OP_POLICY && v == tok_vec) {
+                                const int at = (tok + row.lead) % E;
+#pragma unroll
+                                for (int e = 0; e < E; ++e)
+                                    if (e == at) y[e] += k2;
+                            }
+                            row.store(v, y, act);
+                        }
+                    },
+                    [&](int slot) {
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(empty + 8 * slot);
+                    });
+                if constexpr (OP == OP_DISTILL) {
+                    // the teacher's tokens again, each by the warp that stored its vector
+                    const TeacherList& list = sh.list[s];
+                    if (!info.bad && !isnan(res.lse) && !res.empty)
+                        for (int k = lane; k < info.n_own; k += 32) {
+                            const int at = list.own[k], id = list.id[at];
+                            if (((id + row.lead) / E - first) % plan.chunk / 32 % kWarps != warp) continue;
+                            float q = list.q[at];
+                            if (info.repeats) {
+                                q = 0.f;
+                                for (int p = 0; p < info.n_own; ++p)
+                                    if (list.id[list.own[p]] == id) q += list.q[list.own[p]];
+                            }
+                            const float d = fmaf(c, list.x[at] - res.m, -res.log2_s);
+                            row.dx[id] = from_f32<T>((exp2_approx(d) - q) * k0);
+                        }
+                }
+            }
+            if constexpr (TOP) {
+                const int turn = live_b / cta_n & 1;
+                const uint32_t to = live_b % cta_n;
+                if (rank == to && tid == 0) mbar_expect(smem_addr(&sh.full[turn]), cta_n * a.k * 8);
+                send_best(slice, row, a.k, max_b, isnan(res.lse) ? INFINITY : bound, sh, turn, rank, to);
+                slice.template each<1>([](int) {}, [](Count<1>, const uint4*, int, bool) {},
+                                       [&](int slot) { if (lane == 0) mbar_arrive(empty + 8 * slot); });
+                if (rank == to) {
+                    mbar_wait(smem_addr(&sh.full[turn]), live_b / (2 * cta_n) & 1, &sm.dead);
+                    merge_best(a, i, cta_n, res, sh, turn);
+                }
+            }
+            if (RES) slot_b = (slot_b + (slice.n + plan.chunk - 1) / plan.chunk) % plan.chunks;
+            ++live_b;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(info_empty + 8 * s);
+        };
+
+        if (plan.ahead) {
+            for (int64_t q = 0; q <= rows; ++q) {
+                max_b = max_a;
+                if (q < rows) statistics(q);
+                if (q > 0) rest(q - 1);
+            }
+        } else {
+            for (int64_t q = 0; q < rows; ++q) {
+                statistics(q);
+                max_b = max_a;
+                rest(q);
+            }
+        }
+    }
+    __syncwarp();
+    cluster_arrive();  // (nothing is sent to a CTA that has ended)
+    cluster_wait();
+}
+
+// ---------------------------------------------------------------- backward --
+constexpr int kBackThreads = 256;
+constexpr int kBackVecs = 4;  // a thread's, all loaded before the first is used
+
+template <typename T, bool ENT>
+__global__ void __launch_bounds__(kBackThreads) backward_kernel(const RowArgs a, int ctas_per_row) {
+    constexpr int E = Vec<T>::E;
+    const int64_t i = blockIdx.x / ctas_per_row;
+    const int first = (int)(blockIdx.x % ctas_per_row) * kBackThreads * kBackVecs + threadIdx.x;
+    const Row<T> row(a, i);
+    const int32_t tok = a.tokens ? a.tokens[i] : 0;
+    if (tok < 0) {
+        const float zero[E] = {};
+#pragma unroll
+        for (int u = 0; u < kBackVecs; ++u) row.store(first + u * kBackThreads, zero, first + u * kBackThreads < row.n_vec);
         return;
     }
-    const float w = a.weight ? a.weight[i] : 1.f;
-    if (OP == OP_POLICY) {
-        float g;
-        const float logp = tok < V ? r.logp(x_tok) : NAN;
-        const float term = policy_term(logp, a.advantage[i], a.old_logp, i, a.clip_low, a.clip_high, g);
-        const float beta = a.entropy_coef;
-        __syncthreads();  // x_tok read by everyone before an in-place gradient
-        if (tid == 0) {
-            a.loss[i] = w * (term - beta * r.entropy);
-            if (a.logp) a.logp[i] = logp;
-            if (a.entropy) a.entropy[i] = r.entropy;
-        }
-        if (!a.dx) return;
-        for (int j = tid; j < V; j += kThreads) {
-            const float lp = r.logp(to_f32(x[j])), p = exp2_approx(lp * kLog2e);
-            float d = g * ((j == tok ? 1.f : 0.f) - p) + beta * p * (fmaxf(lp, -1e30f) + r.entropy);
-            dx[j] = from_f32<T>(r.empty && !isnan(g) ? 0.f : d * w * inv_t);
-        }
-        return;
+    uint4 r[kBackVecs];
+#pragma unroll
+    for (int u = 0; u < kBackVecs; ++u)
+        r[u] = first + u * kBackThreads < row.n_vec ? row.load(first + u * kBackThreads) : make_uint4(0, 0, 0, 0);
+    const float inv_t = 1.f / a.temperature;
+    float lse = a.lse_in[i], k0 = 0.f, k1 = 0.f, k2 = 0.f;  // gradient p (k0 + k1 ln p) + [j = token] k2
+    if (a.dlogp) {
+        k2 = a.dlogp[i] * inv_t;
+        k0 = tok < row.vocab ? -k2 : NAN;
     }
-    // distillation
-    float loss = 0.f;
-    const float log2_q = log2f(q_sum);
-    bool bad = q_bad || isnan(r.lse);
-    for (int k = tid; k < a.k; k += kThreads) {
-        const int32_t id = a.teacher_ids[i * a.k + k];
-        if (id < 0) continue;
-        const float lq = c * (load_value(a.teacher_logits, i * a.k + k, a.teacher_dtype) - q_max) - log2_q, q = exp2_approx(lq);
-        if (q > 0.f && id >= V) bad = true;
-        if (q > 0.f && id < V) loss += q * (kLn2 * lq - r.logp(to_f32(x[id])));
+    if (ENT) {
+        const float gh = a.dentropy[i] * inv_t;
+        k0 -= gh * a.entropy_in[i];
+        k1 = -gh;
     }
-    loss = block_reduce(loss, [](float p, float q) { return p + q; }, sh_f);
-    bad = __syncthreads_or(bad);
-    if (tid == 0) a.loss[i] = bad ? NAN : w * loss;
-    if (!a.dx) return;
-    for (int j = tid; j < V; j += kThreads) {
-        float p = exp2_approx(r.logp(to_f32(x[j])) * kLog2e);
-        for (int k = 0; k < a.k; ++k)
-            if (a.teacher_ids[i * a.k + k] == j)
-                p -= exp2_approx(c * (load_value(a.teacher_logits, i * a.k + k, a.teacher_dtype) - q_max) - log2_q);
-        dx[j] = from_f32<T>(bad ? NAN : r.empty ? 0.f : p * w * inv_t);
+    if (lse == kNegInf) {  // -inf logits only: p = 0
+        lse = 0.f;
+        k2 = 0.f;
+    }
+    const int tok_vec = a.dlogp && tok < row.vocab ? (tok + row.lead) / E : -1;
+#pragma unroll
+    for (int u = 0; u < kBackVecs; ++u) {
+        const int v = first + u * kBackThreads;
+        float x[E];
+        Vec<T>::unpack(r[u], x);
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+            const F2 lp = fma2(F2(x[e], x[e + 1]), F2(inv_t, inv_t), F2(-lse, -lse));
+            float l0, l1, d0, d1;
+            lp.get(l0, l1);
+            (lp * F2(kLog2e, kLog2e)).get(d0, d1);
+            const F2 p(exp2_approx(d0), exp2_approx(d1));
+            (p * (ENT ? fma2(F2(k1, k1), F2(fmaxf(l0, -1e30f), fmaxf(l1, -1e30f)), F2(k0, k0)) : F2(k0, k0))).get(x[e], x[e + 1]);
+        }
+        if (v == tok_vec) {
+            const int at = (tok + row.lead) % E;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (e == at) x[e] += k2;
+        }
+        row.store(v, x, v < row.n_vec);
     }
 }
 
-template <int OP>
-cudaError_t launch(const RowArgs& a, cudaStream_t s) {
-    if (a.dtype == TP_F32)
-        row_kernel<float, OP><<<a.n, kThreads, 0, s>>>(a);
-    else if (a.dtype == TP_F16)
-        row_kernel<__half, OP><<<a.n, kThreads, 0, s>>>(a);
-    else
-        row_kernel<__nv_bfloat16, OP><<<a.n, kThreads, 0, s>>>(a);
+// ---------------------------------------------------------------- launches --
+template <typename F>
+cudaError_t by_type(const RowArgs& a, F f) {
+    if (a.dtype == TP_F32) return f(float{});
+    if (a.dtype == TP_F16) return f(__half{});
+    return f(__nv_bfloat16{});
+}
+
+// The cluster and ring of a call. A row's slice of at most kRing / 3 bytes leaves
+// room for the next row's and a part of the one after; fewer CTAs a row exchange less.
+constexpr int kSms = 152;
+constexpr int kMaxChunkVecs = 1024;
+
+template <typename T, int OP, bool RES, bool ENT>
+cudaError_t launch_rows(const RowArgs& a, cudaStream_t s) {
+    constexpr int E = Vec<T>::E;
+    constexpr int kRing = 232448 - (int)sizeof(RowShared) - (int)sizeof(typename OpShared<OP, RES>::type) - 1024;
+    // (rows that all begin in a line of their own have one vector less than rows at any place)
+    const bool lines = (uintptr_t)a.x % 16 == 0 && (a.n == 1 || a.x_stride % E == 0);
+    const int n_vec = (a.vocab + (lines ? 1 : 2) * (E - 1)) / E;
+    Plan plan;
+    plan.cta_n = 1;
+    while (plan.cta_n < kMaxCluster) {
+        const int64_t slice = (int64_t)(n_vec + plan.cta_n - 1) / plan.cta_n * 16;
+        if (!(RES && slice > kRing / 3) && !((int64_t)a.n * plan.cta_n * 2 <= kSms && slice > 8192)) break;
+        plan.cta_n *= 2;
+    }
+    plan.per_cta = (n_vec + plan.cta_n - 1) / plan.cta_n;
+    const int parts = std::max(1, (plan.per_cta + kMaxChunkVecs / 4) / kMaxChunkVecs);
+    plan.chunk = ((plan.per_cta + parts - 1) / parts + 31) / 32 * 32;
+    plan.chunks = std::min(kMaxChunks, kRing / (plan.chunk * 16));
+    const int own = (plan.per_cta + plan.chunk - 1) / plan.chunk;
+    plan.ahead = !RES || 2 * own <= plan.chunks;
+    if (RES && own > plan.chunks) return cudaErrorInvalidValue;
+    auto kernel = wide_kernel<T, OP, RES, ENT>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRing);
+    if (e != cudaSuccess) return e;
+    static const int kClusters[4] = {152, 76, 36, 15};  // of 1, 2, 4 and 8 CTAs that the GPU holds at once
+    const int at = plan.cta_n == 1 ? 0 : plan.cta_n == 2 ? 1 : plan.cta_n == 4 ? 2 : 3;
+    const int64_t clusters = std::min<int64_t>(a.n, kClusters[at]);
+    cudaLaunchAttribute attr[1] = {};
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = plan.cta_n;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(clusters * plan.cta_n));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = (size_t)plan.chunks * plan.chunk * 16;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, a, plan);
+}
+
+template <typename T, bool ENT>
+cudaError_t launch_back(const RowArgs& a, cudaStream_t s) {
+    constexpr int E = Vec<T>::E, per_cta = kBackThreads * kBackVecs;
+    const int ctas = ((a.vocab + 2 * E - 2) / E + per_cta - 1) / per_cta;
+    backward_kernel<T, ENT><<<(unsigned)(a.n * ctas), kBackThreads, 0, s>>>(a, ctas);
     return cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t launch_token_logprobs(const RowArgs& a, cudaStream_t s) { return launch<OP_LOGPROBS>(a, s); }
-cudaError_t launch_token_logprobs_backward(const RowArgs& a, cudaStream_t s) { return launch<OP_BACKWARD>(a, s); }
-cudaError_t launch_policy_loss(const RowArgs& a, cudaStream_t s) { return launch<OP_POLICY>(a, s); }
-cudaError_t launch_distill_loss(const RowArgs& a, cudaStream_t s) { return launch<OP_DISTILL>(a, s); }
+cudaError_t launch_token_logprobs(const RowArgs& a, cudaStream_t s) {
+    return by_type(a, [&](auto t) {
+        typedef decltype(t) T;
+        return a.k > 0 ? launch_rows<T, OP_LOGPROBS, true, true>(a, s) : launch_rows<T, OP_LOGPROBS, false, true>(a, s);
+    });
+}
+
+cudaError_t launch_token_logprobs_backward(const RowArgs& a, cudaStream_t s) {
+    return by_type(a, [&](auto t) {
+        typedef decltype(t) T;
+        return a.dentropy ? launch_back<T, true>(a, s) : launch_back<T, false>(a, s);
+    });
+}
+
+cudaError_t launch_policy_loss(const RowArgs& a, cudaStream_t s) {
+    const bool ent = a.entropy || a.entropy_coef != 0.f;
+    return by_type(a, [&](auto t) {
+        typedef decltype(t) T;
+        if (a.dx) return ent ? launch_rows<T, OP_POLICY, true, true>(a, s) : launch_rows<T, OP_POLICY, true, false>(a, s);
+        return ent ? launch_rows<T, OP_POLICY, false, true>(a, s) : launch_rows<T, OP_POLICY, false, false>(a, s);
+    });
+}
+
+cudaError_t launch_distill_loss(const RowArgs& a, cudaStream_t s) {
+    return by_type(a, [&](auto t) {
+        typedef decltype(t) T;
+        return a.dx ? launch_rows<T, OP_DISTILL, true, false>(a, s) : launch_rows<T, OP_DISTILL, false, false>(a, s);
+    });
+}
 
 }  // namespace tp
