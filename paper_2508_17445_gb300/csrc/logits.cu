@@ -32,7 +32,7 @@ namespace tp {
 namespace {
 
 constexpr int kMaxCluster = 8;
-constexpr int kWarps = 8;            // that work on a row's elements
+constexpr int kWarps = 16;           // that work on a row's elements
 constexpr int kCopyWarp = kWarps;    // issues the bulk copies
 constexpr int kHelpers = 4;          // warps that look ahead at the rows' own values
 constexpr int kThreads = (kWarps + 1 + kHelpers) * 32;
@@ -262,23 +262,23 @@ struct Row {
         return whole(v) ? __ldcs((const uint4*)(x + (v * E - lead))) : load_part(v);
     }
     // Elements e0 .. e1 - 1 of vector v, by element.
-    __device__ __forceinline__ void store_part(int v, const float* f, int e0, int e1) const {
+    __device__ __forceinline__ void store_part(int v, const uint4& r, int e0, int e1) const {
         const int j0 = v * E - lead;
+        const T* t = (const T*)&r;
 #pragma unroll
         for (int e = 0; e < E; ++e)
-            if (e >= e0 && e < e1 && j0 + e >= 0 && j0 + e < vocab) dx[j0 + e] = from_f32<T>(f[e]);
+            if (e >= e0 && e < e1 && j0 + e >= 0 && j0 + e < vocab) dx[j0 + e] = t[e];
     }
     // All lanes of a warp, which hold neighbouring vectors; act: this lane's is one of the row's.
-    __device__ __forceinline__ void store(int v, const float* f, bool act) const {
+    __device__ __forceinline__ void store(int v, const uint4& own, bool act) const {
         if (shift == 0) {
             if (act && whole(v))
-                *(uint4*)(dx + (v * E - lead)) = Vec<T>::pack(f);
+                *(uint4*)(dx + (v * E - lead)) = own;
             else if (act)
-                store_part(v, f, 0, E);
+                store_part(v, own, 0, E);
             return;
         }
         // the line that holds the last elements of the lane before and the first of this one
-        const uint4 own = Vec<T>::pack(f);
         uint32_t w[8] = {__shfl_up_sync(0xffffffffu, own.x, 1), __shfl_up_sync(0xffffffffu, own.y, 1),
                          __shfl_up_sync(0xffffffffu, own.z, 1), __shfl_up_sync(0xffffffffu, own.w, 1),
                          own.x, own.y, own.z, own.w};
@@ -298,9 +298,9 @@ struct Row {
                 for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], 16);
             *(uint4*)((char*)(dx + (v * E - lead)) - shift) = make_uint4(w[0], w[1], w[2], w[3]);
         } else if (act) {
-            store_part(v, f, 0, split);
+            store_part(v, own, 0, split);
         }
-        if (act && (lane == 31 || !(lines >> (lane + 1) & 1))) store_part(v, f, split, E);
+        if (act && (lane == 31 || !(lines >> (lane + 1) & 1))) store_part(v, own, split, E);
     }
 };
 
@@ -621,15 +621,20 @@ struct RowInfo {
     uint4 edge[2];      // the slice's vectors that the row shares with its neighbours, the first and the last
 };
 
+// The teacher's list of one row, k long each; it lies behind the ring.
 struct TeacherList {
-    int32_t id[TP_MAX_TEACHER_LOGITS];   // -1: no share
-    float q[TP_MAX_TEACHER_LOGITS];
-    float x[TP_MAX_TEACHER_LOGITS];      // the student's logits (the first CTA's, and of the slice's tokens)
-    int16_t own[TP_MAX_TEACHER_LOGITS];  // places of the slice's tokens
+    int32_t* id;   // -1: no share
+    float* q;
+    float* x;      // the student's logits (the first CTA's, and of the slice's tokens)
+    int32_t* own;  // places of the slice's tokens
+
+    __device__ __forceinline__ TeacherList(uint8_t* at, int k) {
+        id = (int32_t*)at, q = (float*)(id + k), x = q + k, own = (int32_t*)(x + k);
+    }
+    static constexpr int kBytes = 16;  // an entry
 };
 constexpr int kSeenWords = 256;
 struct TeacherShared {
-    TeacherList list[kSlots];
     uint32_t seen[kHelpers][kSeenWords];  // a bit for the tokens of equal residue
 };
 struct NoShared {};
@@ -679,7 +684,7 @@ __device__ __forceinline__ void keep_edge(RowInfo& info, T x) {
 // A helper warp's look ahead at one row of a distillation: the teacher's shares.
 template <typename T>
 __device__ void teacher_ahead(const RowArgs& a, int64_t i, const Row<T>& row, int first, int n, uint32_t rank, RowInfo& info,
-                              TeacherList& list, uint32_t* seen) {
+                              const TeacherList& list, uint32_t* seen) {
     const int lane = threadIdx.x & 31;
     const float c = kLog2e / a.temperature;
     const int32_t* ids = a.teacher_ids + i * a.k;
@@ -722,7 +727,7 @@ __device__ void teacher_ahead(const RowArgs& a, int64_t i, const Row<T>& row, in
                 id = own ? id : -1;
             }
             const uint32_t owners = __ballot_sync(0xffffffffu, id >= 0);
-            if (id >= 0) list.own[n_own + __popc(owners & ((1u << lane) - 1))] = (int16_t)k;
+            if (id >= 0) list.own[n_own + __popc(owners & ((1u << lane) - 1))] = k;
             n_own += __popc(owners);
         }
         __syncwarp();
@@ -758,6 +763,9 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     const uint32_t full = smem_addr(sm.full), empty = smem_addr(sm.empty);
     const uint32_t info_full = smem_addr(sm.info_full), info_empty = smem_addr(sm.info_empty);
     const uint32_t parts_full = smem_addr(sm.parts_full);
+    auto list_at = [&](int slot) {
+        return TeacherList(ring + plan.chunks * slot_bytes + slot * a.k * TeacherList::kBytes, a.k);
+    };
     if (tid == 0) {
         for (int k = 0; k < plan.chunks; ++k) {
             mbar_init(full + 8 * k, 1);
@@ -790,7 +798,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
                 const T edge = edge_element(row, first, plan.per_cta);
                 mbar_wait(info_empty + 8 * h, (q / kSlots & 1) ^ 1, &sm.dead);
                 keep_edge(sm.info[h], edge);
-                teacher_ahead(a, i, row, first, max(0, min(plan.per_cta, row.n_vec - first)), rank, sm.info[h], sh.list[h], sh.seen[h]);
+                teacher_ahead(a, i, row, first, max(0, min(plan.per_cta, row.n_vec - first)), rank, sm.info[h], list_at(h), sh.seen[h]);
                 if (lane == 0) mbar_arrive(info_full + 8 * h);
             }
         } else {
@@ -924,7 +932,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             const bool tells = rank == 0 && tid == 0;  // writes the row's own results
             if (!info.live) {
                 if constexpr (RES && OP != OP_LOGPROBS) {
-                    const float zero[E] = {};
+                    const uint4 zero = make_uint4(0, 0, 0, 0);
                     for (int g = warp * 32; g < slice.n; g += kRowThreads) row.store(first + g + lane, zero, g + lane < slice.n);
                 }
                 if (tells) {
@@ -1000,12 +1008,12 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
                 const float wt = info.w * inv_t;
                 k0 = wt * (ENT ? a.entropy_coef * res.entropy - g : -g);
                 k1 = ENT ? wt * a.entropy_coef * kLn2 : 0.f;
-                k2 = res.empty ? 0.f : wt * g;
+                k2 = wt * g;
             }
             if constexpr (OP == OP_DISTILL) {
                 k0 = info.bad ? NAN : info.w * inv_t;
                 if (rank == 0 && warp == kWarps - 1) {
-                    const TeacherList& list = sh.list[s];
+                    const TeacherList list = list_at(s);
                     float part = 0.f;
                     if (!info.bad)
                         for (int k = lane; k < a.k; k += 32)
@@ -1015,14 +1023,16 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
                 }
             }
             if constexpr (RES && OP != OP_LOGPROBS) {
-                const int tok_vec = OP == OP_POLICY && tok < row.vocab ? (tok + row.lead) / E : -1;
                 const F2 base(-res.m, -res.m), c2(c, c), less(-res.log2_s, -res.log2_s), k02(k0, k0), k12(k1, k1);
+                // ahead of the warp's first whole vector, and of the first after its last
+                const int plain_lo = row.whole_lo + lane, plain_hi = row.whole_lo + row.whole_n + lane - 31;
                 slice.template each<2>(
                     [](int) {},
-                    [&](auto count, const uint4* r, int v0, bool act) {
+                    [&](auto count, const uint4* r, int v, bool act) {
+                        constexpr int N = decltype(count)::n;
+                        uint4 out[N];
 #pragma unroll
-                        for (int u = 0; u < decltype(count)::n; ++u) {
-                            const int v = v0 + u * kRowThreads;
+                        for (int u = 0; u < N; ++u) {
                             float y[E];
                             Vec<T>::unpack(r[u], y);
 #pragma unroll
@@ -1032,26 +1042,38 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
                                 const F2 p(exp2_approx(d0), exp2_approx(d1));
                                 (p * (ENT ? fma2(k12, F2(fmaxf(d0, -1e30f), fmaxf(d1, -1e30f)), k02) : k02)).get(y[e], y[e + 1]);
                             }
-                            if (OP == OP_POLICY && v == tok_vec) {
-                                const int at = (tok + row.lead) % E;
+                            out[u] = Vec<T>::pack(y);
+                        }
+                        T* dst = row.dx + ((int64_t)v * E - row.lead);
+                        static_assert(N <= 2);
+                        if (row.shift == 0 && v >= plain_lo && v + (N - 1) * kRowThreads < plain_hi) {
 #pragma unroll
-                                for (int e = 0; e < E; ++e)
-                                    if (e == at) y[e] += k2;
-                            }
-                            row.store(v, y, act);
+                            for (int u = 0; u < N; ++u)
+                                if (N > 1 || act) *(uint4*)(dst + u * kRowThreads * E) = out[u];
+                        } else {
+#pragma unroll 1
+                            for (int u = 0; u < N; ++u) row.store(v + u * kRowThreads, u == 0 ? out[0] : out[N - 1], act);
                         }
                     },
                     [&](int slot) {
                         __syncwarp();
                         if (lane == 0) mbar_arrive(empty + 8 * slot);
                     });
+                // the tokens that have a term of their own again, each by the warp that stored its vector
+                auto owner = [&](int id) { return ((id + row.lead) / E - first) % plan.chunk / 32 % kWarps; };
+                if constexpr (OP == OP_POLICY) {
+                    const int v = (tok + row.lead) / E - first;
+                    if (lane == 0 && tok < row.vocab && v >= 0 && v < slice.n && !res.empty && owner(tok) == warp) {
+                        const float d = fmaf(c, info.x_tok - res.m, -res.log2_s), p = exp2_approx(d);
+                        row.dx[tok] = from_f32<T>(fmaf(p, ENT ? fmaf(k1, fmaxf(d, -1e30f), k0) : k0, k2));
+                    }
+                }
                 if constexpr (OP == OP_DISTILL) {
-                    // the teacher's tokens again, each by the warp that stored its vector
-                    const TeacherList& list = sh.list[s];
+                    const TeacherList list = list_at(s);
                     if (!info.bad && !isnan(res.lse) && !res.empty)
                         for (int k = lane; k < info.n_own; k += 32) {
                             const int at = list.own[k], id = list.id[at];
-                            if (((id + row.lead) / E - first) % plan.chunk / 32 % kWarps != warp) continue;
+                            if (owner(id) != warp) continue;
                             float q = list.q[at];
                             if (info.repeats) {
                                 q = 0.f;
@@ -1112,7 +1134,7 @@ __global__ void __launch_bounds__(kBackThreads) backward_kernel(const RowArgs a,
     const Row<T> row(a, i);
     const int32_t tok = a.tokens ? a.tokens[i] : 0;
     if (tok < 0) {
-        const float zero[E] = {};
+        const uint4 zero = make_uint4(0, 0, 0, 0);
 #pragma unroll
         for (int u = 0; u < kBackVecs; ++u) row.store(first + u * kBackThreads, zero, first + u * kBackThreads < row.n_vec);
         return;
@@ -1157,7 +1179,7 @@ __global__ void __launch_bounds__(kBackThreads) backward_kernel(const RowArgs a,
             for (int e = 0; e < E; ++e)
                 if (e == at) x[e] += k2;
         }
-        row.store(v, x, v < row.n_vec);
+        row.store(v, Vec<T>::pack(x), v < row.n_vec);
     }
 }
 
@@ -1169,15 +1191,16 @@ cudaError_t by_type(const RowArgs& a, F f) {
     return f(__nv_bfloat16{});
 }
 
-// The cluster and ring of a call. A row's slice of at most kRing / 3 bytes leaves
+// The cluster and ring of a call. A row's slice of at most a third of the ring bytes leaves
 // room for the next row's and a part of the one after; fewer CTAs a row exchange less.
 constexpr int kSms = 152;
-constexpr int kMaxChunkVecs = 1024;
+constexpr int kMaxChunkVecs = 2048;
 
 template <typename T, int OP, bool RES, bool ENT>
 cudaError_t launch_rows(const RowArgs& a, cudaStream_t s) {
     constexpr int E = Vec<T>::E;
-    constexpr int kRing = 232448 - (int)sizeof(RowShared) - (int)sizeof(typename OpShared<OP, RES>::type) - 1024;
+    constexpr int kMost = 232448 - (int)sizeof(RowShared) - (int)sizeof(typename OpShared<OP, RES>::type) - 1024;
+    const int lists = OP == OP_DISTILL ? kSlots * a.k * TeacherList::kBytes : 0, room = kMost - lists;
     // (rows that all begin in a line of their own have one vector less than rows at any place)
     const bool lines = (uintptr_t)a.x % 16 == 0 && (a.n == 1 || a.x_stride % E == 0);
     const int n_vec = (a.vocab + (lines ? 1 : 2) * (E - 1)) / E;
@@ -1185,18 +1208,18 @@ cudaError_t launch_rows(const RowArgs& a, cudaStream_t s) {
     plan.cta_n = 1;
     while (plan.cta_n < kMaxCluster) {
         const int64_t slice = (int64_t)(n_vec + plan.cta_n - 1) / plan.cta_n * 16;
-        if (!(RES && slice > kRing / 3) && !((int64_t)a.n * plan.cta_n * 2 <= kSms && slice > 8192)) break;
+        if (!(RES && slice > room / 3) && !((int64_t)a.n * plan.cta_n * 2 <= kSms && slice > 8192)) break;
         plan.cta_n *= 2;
     }
     plan.per_cta = (n_vec + plan.cta_n - 1) / plan.cta_n;
     const int parts = std::max(1, (plan.per_cta + kMaxChunkVecs / 4) / kMaxChunkVecs);
     plan.chunk = ((plan.per_cta + parts - 1) / parts + 31) / 32 * 32;
-    plan.chunks = std::min(kMaxChunks, kRing / (plan.chunk * 16));
+    plan.chunks = std::min(kMaxChunks, room / (plan.chunk * 16));
     const int own = (plan.per_cta + plan.chunk - 1) / plan.chunk;
     plan.ahead = !RES || 2 * own <= plan.chunks;
     if (RES && own > plan.chunks) return cudaErrorInvalidValue;
     auto kernel = wide_kernel<T, OP, RES, ENT>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRing);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
     if (e != cudaSuccess) return e;
     static const int kClusters[4] = {152, 76, 36, 15};  // of 1, 2, 4 and 8 CTAs that the GPU holds at once
     const int at = plan.cta_n == 1 ? 0 : plan.cta_n == 2 ? 1 : plan.cta_n == 4 ? 2 : 3;
@@ -1208,7 +1231,7 @@ cudaError_t launch_rows(const RowArgs& a, cudaStream_t s) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(clusters * plan.cta_n));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = (size_t)plan.chunks * plan.chunk * 16;
+    cfg.dynamicSmemBytes = (size_t)plan.chunks * plan.chunk * 16 + lists;
     cfg.stream = s;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
