@@ -10,11 +10,13 @@
 // All of it is bound by HBM: 8 to 20 operations an element against its 2 or 4
 // bytes, so a row is read once. wide_kernel is persistent: a cluster of CTAs takes
 // row after row, each CTA a slice of it, which bulk copies bring into a ring of
-// chunks in shared memory. Sixteen warps take the slice's statistics, send them to
-// every CTA of the cluster through distributed shared memory and, while these
-// travel, begin the next row; then they make the gradient (or find the
-// alternatives) from the same chunks and give them back to the ring. Nothing
-// waits for a whole CTA. backward_kernel needs no statistics and streams.
+// chunks in shared memory. Sixteen warps take the slice's statistics and send them
+// to every CTA of the cluster through distributed shared memory. A helper warp,
+// which had looked up the row's own values before its turn, joins them, writes the
+// row's results and leaves the gradient's coefficients, while the sixteen are at
+// the next row; then these make the gradient from the same chunks and give them
+// back to the ring. Nothing waits for a whole CTA. backward_kernel needs no
+// statistics and streams.
 //
 // Rows start at any element: 16-byte vectors are counted from the line that the
 // row's logits begin in, and the two vectors at the ends that a row shares with
@@ -240,6 +242,7 @@ struct Row {
     int whole_lo, whole_n;  // vectors whole_lo .. whole_lo + whole_n - 1 hold E elements of the row
     int shift;              // bytes by which the gradient's vectors begin after a line
 
+    Row() = default;
     __device__ __forceinline__ Row(const RowArgs& a, int64_t i) {
         x = (const T*)a.x + i * a.x_stride;
         dx = a.dx ? (T*)a.dx + i * a.dx_stride : nullptr;
@@ -405,223 +408,39 @@ __device__ __forceinline__ float load_value(const void* p, int64_t i, int dtype)
     return __bfloat162float(((const __nv_bfloat16*)p)[i]);
 }
 
-// ------------------------------------------------------------ alternatives --
-// The k largest logits of a row, of equal ones the lower id first. A key holds
-// both: the logit in an order of unsigned integers above the complement of its id.
-// Each CTA keeps the k largest keys of its slice, the first CTA merges them.
-//
-// A thread's maximum is known from the statistics. Where each of a CTA's W warps
-// has ceil(k / W) lanes whose maximum is at least b, the CTA has k logits that are,
-// so nothing below the largest b of the cluster's CTAs is among the row's k. What
-// is not below it is a short list in all but contrived rows (few distinct values,
-// all large logits in one thread's places); where it is longer than kList, the
-// CTA finds its k-th largest key exactly, by digits.
-constexpr int kList = 256;
-
-typedef unsigned long long Key;
-
-__device__ __forceinline__ Key make_key(float x, int id) {
-    const uint32_t b = __float_as_uint(x + 0.f);  // -0 as +0
-    return (Key)(b & 0x80000000u ? ~b : b | 0x80000000u) << 32 | (0xffffffffu - (uint32_t)id);
-}
-__device__ __forceinline__ int key_id(Key k) { return (int)(0xffffffffu - (uint32_t)k); }
-__device__ __forceinline__ float key_value(Key k) {
-    const uint32_t u = (uint32_t)(k >> 32);
-    return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
-}
-
-struct TopShared {
-    Key list[kList];
-    Key best[2][kMaxCluster][TP_MAX_ALTERNATIVES];  // where this CTA merges: each CTA's keys, descending, 0 where none is left
-    uint64_t full[2];                               // best's barriers
-    int n, digit, rest;
-    int hist[256];
-};
-
-// One row's chunks in the ring, as the working warps see them: groups of 32
-// vectors, group g of a chunk is warp (g % kWarps)'s.
-template <int N>
-struct Count {
-    static constexpr int n = N;
-};
-template <typename T>
-struct Slice {
-    static constexpr int E = Vec<T>::E;
-    const uint8_t* ring;
-    int slot, slots, slot_bytes;  // the first chunk's
-    int first, n, chunk;          // the slice's first vector, its vectors, a chunk's
-
-    // f(Count<M>, vectors read (M, kRowThreads apart), the first's number in the row, act), M = N or 1;
-    // wait(slot) before a chunk, done(slot) after it.
-    template <int N, typename W, typename F, typename D>
-    __device__ __forceinline__ void each(W wait, F f, D done) const {
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-        int at = slot;
-        for (int v0 = 0; v0 < n; v0 += chunk) {
-            wait(at);
-            const uint4* data = (const uint4*)(ring + (size_t)at * slot_bytes) + lane;
-            const int m = min(chunk, n - v0), v = first + v0 + lane;
-            int g = warp * 32;
-            for (; g + (N - 1) * kRowThreads + 32 <= m; g += N * kRowThreads) {
-                uint4 r[N];
-#pragma unroll
-                for (int u = 0; u < N; ++u) r[u] = data[g + u * kRowThreads];
-                f(Count<N>{}, r, v + g, true);
-            }
-            for (; g < m; g += kRowThreads) {
-                uint4 r = make_uint4(Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone);
-                const bool act = g + lane < m;
-                if (act) r = data[g];
-                f(Count<1>{}, &r, v + g, act);
-            }
-            done(at);
-            if (++at == slots) at = 0;
-        }
-    }
-    // f(logit, id) for every logit above -inf of this thread's vectors.
-    template <typename F>
-    __device__ __forceinline__ void each_logit(const Row<T>& row, F f) const {
-        each<1>([](int) {}, [&](Count<1>, const uint4* r, int v, bool) {
-            float x[E];
-            Vec<T>::unpack(r[0], x);
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (x[e] > kNegInf) f(x[e], v * E + e - row.lead);
-        }, [](int) {});
-    }
-};
-
-// The k-th largest key of the slice by its digits of 8 bits, the highest first
-// (0 if there are fewer). The id's highest digit is the same in all.
-template <typename T>
-__device__ Key kth_key(const Slice<T>& slice, const Row<T>& row, int k, TopShared& sh) {
-    Key found = 0, mask = 0;
-    int rest = k;
-    for (int shift = 56; shift >= 0; shift -= 8) {
-        if (shift == 24) {
-            found |= (Key)0xff << 24;
-            mask |= (Key)0xff << 24;
-            continue;
-        }
-        for (int b = threadIdx.x; b < 256; b += kRowThreads) sh.hist[b] = 0;
-        row_threads_sync();
-        slice.each_logit(row, [&](float x, int id) {
-            const Key key = make_key(x, id);
-            if ((key & mask) == found) atomicAdd(&sh.hist[(int)(key >> shift) & 255], 1);
-        });
-        row_threads_sync();
-        if (threadIdx.x < 32) {  // lane l: digits 255 - 8 l downwards
-            int own[8], sum = 0;
-            for (int b = 0; b < 8; ++b) sum += own[b] = sh.hist[255 - 8 * threadIdx.x - b];
-            int before = sum;
-            for (int off = 1; off < 32; off <<= 1) {
-                const int o = __shfl_up_sync(0xffffffffu, before, off);
-                if ((int)threadIdx.x >= off) before += o;
-            }
-            if (threadIdx.x == 31) sh.digit = before < rest ? -1 : 0;
-            __syncwarp();
-            before -= sum;
-            if (before < rest && before + sum >= rest) {
-                int b = 0;
-                while (before + own[b] < rest) before += own[b++];
-                sh.digit = 255 - 8 * threadIdx.x - b;
-                sh.rest = rest - before;
-            }
-        }
-        row_threads_sync();
-        if (sh.digit < 0) return 0;
-        found |= (Key)sh.digit << shift;
-        mask |= (Key)0xff << shift;
-        rest = sh.rest;
-    }
-    return found;
-}
-
-// This CTA's k largest keys, descending, sent to the CTA `to` of the cluster; the
-// working warps. own_max: the thread's largest logit; bound: see above.
-template <typename T>
-__device__ void send_best(const Slice<T>& slice, const Row<T>& row, int k, float own_max, float bound, TopShared& sh, int turn,
-                          uint32_t rank, uint32_t to) {
-    if (threadIdx.x == 0) sh.n = 0;
-    row_threads_sync();
-    if (__any_sync(0xffffffffu, own_max >= bound))
-        slice.each_logit(row, [&](float x, int id) {
-            if (x >= bound) {
-                const int at = atomicAdd(&sh.n, 1);
-                if (at < kList) sh.list[at] = make_key(x, id);
-            }
-        });
-    row_threads_sync();
-    if (sh.n > kList) {
-        const Key kth = kth_key(slice, row, k, sh);
-        if (threadIdx.x == 0) sh.n = 0;
-        row_threads_sync();
-        slice.each_logit(row, [&](float x, int id) {
-            const Key key = make_key(x, id);
-            if (key >= kth) {
-                const int at = atomicAdd(&sh.n, 1);
-                if (at < kList) sh.list[at] = key;  // (k of them)
-            }
-        });
-        row_threads_sync();
-    }
-    const int m = min(sh.n, kList);
-    const uint32_t dst = map_to(smem_addr(&sh.best[turn][rank][0]), to), bar = map_to(smem_addr(&sh.full[turn]), to);
-    for (int p = threadIdx.x; p < max(m, k); p += kRowThreads) {
-        if (p >= m) {
-            send(dst + p * 8, bar, 0ull);
-            continue;
-        }
-        const Key key = sh.list[p];
-        int place = 0;
-        for (int q = 0; q < m; ++q) place += sh.list[q] > key;
-        if (place < k) send(dst + place * 8, bar, key);
-    }
-    row_threads_sync();  // the list is free again
-}
-
-// The row's k largest keys, from every CTA's; the working warps.
-__device__ void merge_best(const RowArgs& a, int64_t i, int cta_n, const RowResult& r, const TopShared& sh, int turn) {
-    const int k = a.k;
-    const bool nan = isnan(r.lse);
-    for (int p = threadIdx.x; p < cta_n * k; p += kRowThreads) {
-        const int own = p / k, at = p - own * k;
-        const Key key = sh.best[turn][own][at];
-        int place = at;
-        for (int q = 0; q < cta_n && place < k; ++q) {
-            if (q == own) continue;
-            int lo = 0, hi = k;  // how many of q's come before: larger, or for "none" (0) the lower CTA's
-            while (lo < hi) {
-                const int mid = (lo + hi) / 2;
-                const Key o = sh.best[turn][q][mid];
-                if (o > key || (o == key && q < own))
-                    lo = mid + 1;
-                else
-                    hi = mid;
-            }
-            place += lo;
-        }
-        if (place < k) {
-            const bool some = key != 0 && !nan;
-            a.top_ids[i * k + place] = some ? key_id(key) : -1;
-            a.top_logp[i * k + place] = nan ? NAN : some ? r.logp(key_value(key)) : kNegInf;
-        }
-    }
-}
-
 // --------------------------------------------------------------- the rows --
 enum { OP_LOGPROBS, OP_POLICY, OP_DISTILL };
 
+typedef unsigned long long Key;
+
 // A row's own values, looked up ahead of its turn.
+template <typename T>
 struct RowInfo {
+    Row<T> row;
+    uint4 edge[2];      // the slice's vectors that the row shares with its neighbours, the first and the last
     int32_t live, tok;  // not live: padding
     float x_tok, w, adv, old;
     int32_t bad, n_own; // distillation: the teacher's answer is not one; its tokens in this CTA's slice
     int32_t repeats;    // some of these may come twice
-    uint4 edge[2];      // the slice's vectors that the row shares with its neighbours, the first and the last
 };
 
-// The teacher's list of one row, k long each; it lies behind the ring.
+// What the gradient p (k0 + k1 log2 p) takes; a token that is given adds k2 to its own.
+struct Coef {
+    float m, log2_s, k0, k1, k2;
+    int32_t terms;  // whether tokens have terms of their own
+};
+
+template <typename T>
+struct RowShared {
+    RowInfo<T> info[kSlots];
+    float4 parts[kSlots][kMaxCluster][kWarps];  // statistics (m, s, t) and bound of every warp of the cluster
+    Coef coef[kSlots];
+    uint64_t full[kMaxChunks], empty[kMaxChunks];                                           // of the ring's chunks
+    uint64_t info_full[kSlots], info_empty[kSlots], parts_full[kSlots], coef_full[kSlots];  // of a row's slot
+    int dead;
+};
+
+// The teacher's list of one row, k long each; the slots' lie behind the ring.
 struct TeacherList {
     int32_t* id;   // -1: no share
     float* q;
@@ -633,33 +452,27 @@ struct TeacherList {
     }
     static constexpr int kBytes = 16;  // an entry
 };
-constexpr int kSeenWords = 256;
-struct TeacherShared {
-    uint32_t seen[kHelpers][kSeenWords];  // a bit for the tokens of equal residue
-};
-struct NoShared {};
+constexpr int kSeenWords = 256;  // a bit for the tokens of equal residue, by which repeated ones are told
 
-template <int OP, bool RES>
-struct OpShared {
-    typedef NoShared type;
+// Alternatives. A key holds a logit, in an order of unsigned integers, above the
+// complement of its id: the k largest keys are the k largest logits, of equal ones
+// the lower ids. Where each of a CTA's warps has ceil(k / kWarps) lanes that have
+// met a logit of at least b, nothing below b is among the slice's k. The warps
+// take that b from their lanes' maxima after the first chunk and again after 2, 4,
+// 8, ...; what is not below it goes on the row's list. The helper warp leaves out
+// what the last bound excludes, ranks the rest by comparing all with all, and one
+// CTA's helper merges the cluster's. A list that overflows (many equal logits, or
+// rows in rising order) is made again by finding the k-th largest key by digits.
+constexpr int kList = 1024;
+struct TopShared {
+    Key list[kSlots][kList];
+    Key best[kSlots][kMaxCluster][TP_MAX_ALTERNATIVES];  // the first CTA's: each CTA's keys, descending, 0 where none is left
+    uint64_t best_full[kSlots];
+    float bound[2][kWarps];
+    int n[kSlots];
+    int digit, rest;
+    int hist[256];
 };
-template <>
-struct OpShared<OP_LOGPROBS, true> {
-    typedef TopShared type;
-};
-template <bool RES>
-struct OpShared<OP_DISTILL, RES> {
-    typedef TeacherShared type;
-};
-
-struct RowShared {
-    float4 parts[kSlots][kMaxCluster][kWarps];  // statistics (m, s, t) and bound of every warp of the cluster
-    RowInfo info[kSlots];
-    uint64_t full[kMaxChunks], empty[kMaxChunks];
-    uint64_t info_full[kSlots], info_empty[kSlots], parts_full[kSlots];
-    int dead;
-};
-
 struct Plan {
     int cta_n;          // CTAs a cluster
     int chunk, chunks;  // vectors a chunk, chunks of the ring
@@ -667,6 +480,221 @@ struct Plan {
     int ahead;          // whether a row's statistics are begun before the last row is done
 };
 
+// One row's chunks in the ring, as the working warps see them: groups of 32
+// vectors, group g of a chunk is warp (g % kWarps)'s.
+template <int N>
+struct Count {
+    static constexpr int n = N;
+};
+template <typename T>
+struct Slice {
+    const uint8_t* ring;
+    int slot, slots, slot_bytes;  // the first chunk's
+    int first, n, chunk;          // the slice's first vector, its vectors, a chunk's
+
+    // f(Count<M>, vectors read (M, kRowThreads apart), the first's number in the row, act) with M = N or 1,
+    // over the chunk that begins at vector v0 of the slice.
+    template <int N, typename F>
+    __device__ __forceinline__ void chunk_of(int at, int v0, F f) const {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        const uint4* data = (const uint4*)(ring + at * slot_bytes) + lane;
+        const int m = min(chunk, n - v0), v = first + v0 + lane;
+        int g = warp * 32;
+        for (; g + (N - 1) * kRowThreads + 32 <= m; g += N * kRowThreads) {
+            uint4 r[N];
+#pragma unroll
+            for (int u = 0; u < N; ++u) r[u] = data[g + u * kRowThreads];
+            f(Count<N>{}, r, v + g, true);
+        }
+        for (; g < m; g += kRowThreads) {
+            uint4 r = make_uint4(Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone);
+            const bool act = g + lane < m;
+            if (act) r = data[g];
+            f(Count<1>{}, &r, v + g, act);
+        }
+    }
+    // The same over the slice; wait(slot) before a chunk, done(slot, its number) after it.
+    template <int N, typename W, typename F, typename D>
+    __device__ __forceinline__ void each(W wait, F f, D done) const {
+        int at = slot;
+        for (int v0 = 0, k = 0; v0 < n; v0 += chunk, ++k) {
+            wait(at);
+            chunk_of<N>(at, v0, f);
+            done(at, k);
+            if (++at == slots) at = 0;
+        }
+    }
+};
+
+// ------------------------------------------------------------ alternatives --
+__device__ __forceinline__ Key make_key(float x, int id) {
+    const uint32_t b = __float_as_uint(x + 0.f);  // -0 as +0
+    return (Key)(b & 0x80000000u ? ~b : b | 0x80000000u) << 32 | (0xffffffffu - (uint32_t)id);
+}
+__device__ __forceinline__ int key_id(Key k) { return (int)(0xffffffffu - (uint32_t)k); }
+__device__ __forceinline__ float key_value(Key k) {
+    const uint32_t u = (uint32_t)(k >> 32);
+    return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
+}
+
+// Lane values in descending order; the one at place `at`.
+__device__ __forceinline__ float warp_kth(float v, int at) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll
+        for (int step = size >> 1; step; step >>= 1) {
+            const float o = __shfl_xor_sync(0xffffffffu, v, step);
+            const bool down = (lane & size) == 0, low = (lane & step) == 0;
+            v = down == low ? fmaxf(v, o) : fminf(v, o);
+        }
+    return __shfl_sync(0xffffffffu, v, at);
+}
+
+// Puts the logits of M vectors that are not below the bound on the list.
+template <typename T, int M>
+__device__ __forceinline__ void collect(const uint4* r, int v, int lead, float bound, Key* list, int* n) {
+    constexpr int E = Vec<T>::E;
+#pragma unroll
+    for (int u = 0; u < M; ++u)
+        if (Vec<T>::max_of(r[u]) >= bound) {
+            float x[E];
+            Vec<T>::unpack(r[u], x);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (x[e] >= bound && x[e] > kNegInf) {
+                    const int at = atomicAdd(n, 1);
+                    if (at < kList) list[at] = make_key(x[e], (v + u * kRowThreads) * E + e - lead);
+                }
+        }
+}
+
+// The list of the slice's k largest keys, from memory; all working warps. The
+// k-th largest key is found by its digits of 8 bits, the highest first; the id's
+// highest digit is the same in all.
+template <typename T>
+__device__ __noinline__ void collect_exact(const Row<T>& row, int first, int n, int k, TopShared& sh, Key* list, int* count) {
+    constexpr int E = Vec<T>::E;
+    auto each_key = [&](auto f) {
+        for (int v = first + threadIdx.x; v < first + n; v += kRowThreads) {
+            float x[E];
+            Vec<T>::unpack(row.load(v), x);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (x[e] > kNegInf) f(make_key(x[e], v * E + e - row.lead));
+        }
+    };
+    Key found = 0, mask = 0;
+    int rest = k;
+    for (int shift = 56; shift >= 0; shift -= 8) {
+        if (shift == 24) {
+            found |= (Key)0xff << 24;
+            mask |= (Key)0xff << 24;
+            continue;
+        }
+        for (int b = threadIdx.x; b < 256; b += kRowThreads) sh.hist[b] = 0;
+        row_threads_sync();
+        each_key([&](Key key) {
+            if ((key & mask) == found) atomicAdd(&sh.hist[(int)(key >> shift) & 255], 1);
+        });
+        row_threads_sync();
+        if (threadIdx.x < 32) {  // lane l: digits 255 - 8 l downwards
+            int sum = 0;
+            for (int b = 0; b < 8; ++b) sum += sh.hist[255 - 8 * threadIdx.x - b];
+            int before = sum;
+            for (int off = 1; off < 32; off <<= 1) {
+                const int o = __shfl_up_sync(0xffffffffu, before, off);
+                if ((int)threadIdx.x >= off) before += o;
+            }
+            if (threadIdx.x == 31) sh.digit = 0;  // (more keys than k: the list had overflowed)
+            __syncwarp();
+            before -= sum;
+            if (before < rest && before + sum >= rest) {
+                int b = 0, own = sh.hist[255 - 8 * threadIdx.x];
+                while (before + own < rest) {
+                    before += own;
+                    own = sh.hist[255 - 8 * threadIdx.x - ++b];
+                }
+                sh.digit = 255 - 8 * threadIdx.x - b;
+                sh.rest = rest - before;
+            }
+        }
+        row_threads_sync();
+        found |= (Key)sh.digit << shift;
+        mask |= (Key)0xff << shift;
+        rest = sh.rest;
+    }
+    if (threadIdx.x == 0) *count = 0;
+    row_threads_sync();
+    each_key([&](Key key) {
+        if (key >= found) {
+            const int at = atomicAdd(count, 1);
+            if (at < kList) list[at] = key;  // (k of them)
+        }
+    });
+    row_threads_sync();
+}
+
+// One helper warp: the row's alternatives from the CTAs' lists. bound: the slice's last.
+__device__ __forceinline__ void alternatives(const RowArgs& a, int64_t i, TopShared& sh, int s, uint32_t parity, uint32_t rank, int cta_n,
+                                             float bound, const RowResult& r, volatile int* dead) {
+    const int lane = threadIdx.x & 31, k = a.k;
+    Key* list = sh.list[s];
+    const int met = min(sh.n[s], kList);
+    const Key least = bound > kNegInf ? make_key(bound, 0x7fffffff) : 0;  // of its equals the last
+    int m = 0;
+    for (int p0 = 0; p0 < met; p0 += 32) {  // left out in place: never written ahead of what is read
+        const Key key = p0 + lane < met ? list[p0 + lane] : 0;
+        const uint32_t stays = __ballot_sync(0xffffffffu, key >= least && key != 0);
+        if (stays >> lane & 1) list[m + __popc(stays & ((1u << lane) - 1))] = key;
+        m += __popc(stays);
+        __syncwarp();
+    }
+    const bool nan = isnan(r.lse), alone = cta_n == 1;
+    auto write = [&](int place, Key key) {
+        const bool some = key != 0 && !nan;
+        a.top_ids[i * k + place] = some ? key_id(key) : -1;
+        a.top_logp[i * k + place] = nan ? NAN : some ? r.logp(key_value(key)) : kNegInf;
+    };
+    const uint32_t bar = map_to(smem_addr(&sh.best_full[s]), 0), dst = map_to(smem_addr(&sh.best[s][rank][0]), 0);
+    if (!alone && rank == 0 && lane == 0) mbar_expect(smem_addr(&sh.best_full[s]), cta_n * k * 8);
+    for (int p = lane; p < max(m, k); p += 32) {
+        const Key key = p < m ? list[p] : 0;
+        int place = p;
+        if (p < m) {
+            place = 0;
+            for (int q = 0; q < m; ++q) place += list[q] > key;
+        }
+        if (place >= k) continue;
+        if (alone)
+            write(place, key);
+        else
+            send(dst + place * 8, bar, key);
+    }
+    if (alone || rank != 0) return;
+    mbar_wait(smem_addr(&sh.best_full[s]), parity, dead);
+    for (int p = lane; p < cta_n * k; p += 32) {
+        const int own = p / k, at = p - own * k;
+        const Key key = sh.best[s][own][at];
+        int place = at;
+        for (int q = 0; q < cta_n && place < k; ++q) {
+            if (q == own) continue;
+            int lo = 0, hi = k;  // how many of q's come before: larger, or for "none" (0) the lower CTA's
+            while (lo < hi) {
+                const int mid = (lo + hi) / 2;
+                const Key o = sh.best[s][q][mid];
+                if (o > key || (o == key && q < own))
+                    lo = mid + 1;
+                else
+                    hi = mid;
+            }
+            place += lo;
+        }
+        if (place < k) write(place, key);
+    }
+}
+
+// ----------------------------------------------------------- helper warps --
 // A lane's share of a row's edges: lanes 0 .. E - 1 the first vector's elements, 16 .. the last one's.
 template <typename T>
 __device__ __forceinline__ T edge_element(const Row<T>& row, int first, int per_cta) {
@@ -676,15 +704,15 @@ __device__ __forceinline__ T edge_element(const Row<T>& row, int first, int per_
     return row.x[j];
 }
 template <typename T>
-__device__ __forceinline__ void keep_edge(RowInfo& info, T x) {
+__device__ __forceinline__ void keep_edge(RowInfo<T>& info, T x) {
     const int lane = threadIdx.x & 31, e = lane & 15;
     if (e < Vec<T>::E) ((T*)&info.edge[lane / 16])[e] = x;
 }
 
-// A helper warp's look ahead at one row of a distillation: the teacher's shares.
+// The teacher's shares of one row of a distillation.
 template <typename T>
-__device__ void teacher_ahead(const RowArgs& a, int64_t i, const Row<T>& row, int first, int n, uint32_t rank, RowInfo& info,
-                              const TeacherList& list, uint32_t* seen) {
+__device__ __forceinline__ void teacher_ahead(const RowArgs& a, int64_t i, const Row<T>& row, int first, int n, uint32_t rank,
+                                              RowInfo<T>& info, const TeacherList& list, uint32_t* seen) {
     const int lane = threadIdx.x & 31;
     const float c = kLog2e / a.temperature;
     const int32_t* ids = a.teacher_ids + i * a.k;
@@ -742,29 +770,32 @@ __device__ void teacher_ahead(const RowArgs& a, int64_t i, const Row<T>& row, in
         info.repeats = twice;
         info.w = a.weight ? a.weight[i] : 1.f;
     }
-    __syncwarp();
 }
 
 // RES: the slice stays in the ring until the row's statistics are known, for a
-// gradient or alternatives. ENT: the entropy is asked for (or in the gradient).
-template <typename T, int OP, bool RES, bool ENT>
+// gradient. ENT: the entropy is asked for (or in the gradient). TOP: alternatives.
+template <typename T, int OP, bool RES, bool ENT, bool TOP>
 __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant__ RowArgs a, const __grid_constant__ Plan plan) {
     extern __shared__ __align__(128) uint8_t ring[];
-    __shared__ RowShared sm;
-    __shared__ typename OpShared<OP, RES>::type sh;
-    constexpr bool TOP = OP == OP_LOGPROBS && RES;
+    __shared__ RowShared<T> sm;
     constexpr int E = Vec<T>::E;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int cta_n = plan.cta_n, slot_bytes = plan.chunk * 16;
     const uint32_t rank = cluster_rank();
-    const int64_t groups = gridDim.x / cta_n, group = blockIdx.x / cta_n;
-    const int64_t rows = (a.n - group + groups - 1) / groups;  // row q of the cluster is group + q groups
+    const int groups = gridDim.x / cta_n, group = blockIdx.x / cta_n;
+    const int rows = (a.n - group + groups - 1) / groups;  // row q of the cluster is group + q groups
     const int first = rank * plan.per_cta;
     const uint32_t full = smem_addr(sm.full), empty = smem_addr(sm.empty);
     const uint32_t info_full = smem_addr(sm.info_full), info_empty = smem_addr(sm.info_empty);
-    const uint32_t parts_full = smem_addr(sm.parts_full);
+    const uint32_t parts_full = smem_addr(sm.parts_full), coef_full = smem_addr(sm.coef_full);
+    auto slot_of = [](int q) { return q % kSlots; };
+    auto parity_of = [](int q) { return (uint32_t)(q / kSlots) & 1; };
+    // behind the ring
+    uint8_t* const behind = ring + plan.chunks * slot_bytes;
+    TopShared& sh = *(TopShared*)behind;
+    uint32_t* const seen = (uint32_t*)behind;
     auto list_at = [&](int slot) {
-        return TeacherList(ring + plan.chunks * slot_bytes + slot * a.k * TeacherList::kBytes, a.k);
+        return TeacherList(behind + kHelpers * kSeenWords * 4 + slot * a.k * TeacherList::kBytes, a.k);
     };
     if (tid == 0) {
         for (int k = 0; k < plan.chunks; ++k) {
@@ -775,60 +806,59 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             mbar_init(info_full + 8 * k, 1);
             mbar_init(info_empty + 8 * k, kWarps + 1);
             mbar_init(parts_full + 8 * k, 1);
+            mbar_init(coef_full + 8 * k, 1);
+            if constexpr (TOP) {
+                mbar_init(smem_addr(&sh.best_full[k]), 1);
+                sh.n[k] = 0;
+            }
         }
-        if constexpr (TOP)
-            for (int k = 0; k < 2; ++k) mbar_init(smem_addr(&sh.full[k]), 1);
         sm.dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if constexpr (OP == OP_DISTILL)
-        for (int k = tid; k < kHelpers * kSeenWords; k += kThreads) (&sh.seen[0][0])[k] = 0;
+        for (int k = tid; k < kHelpers * kSeenWords; k += kThreads) seen[k] = 0;
     __syncthreads();
     cluster_arrive();  // every CTA's barriers are there
     cluster_wait();
 
     if (warp > kCopyWarp) {
-        // ---- looking ahead: helper h at rows h, h + kHelpers, ...
-        const int h = warp - kCopyWarp - 1;
+        // ---- helper s: rows s, s + kSlots, ...
         static_assert(kHelpers == kSlots);
-        if constexpr (OP == OP_DISTILL) {
-            for (int64_t q = h; q < rows; q += kHelpers) {
-                const int64_t i = group + q * groups;
-                const Row<T> row(a, i);
-                const T edge = edge_element(row, first, plan.per_cta);
-                mbar_wait(info_empty + 8 * h, (q / kSlots & 1) ^ 1, &sm.dead);
-                keep_edge(sm.info[h], edge);
-                teacher_ahead(a, i, row, first, max(0, min(plan.per_cta, row.n_vec - first)), rank, sm.info[h], list_at(h), sh.seen[h]);
-                if (lane == 0) mbar_arrive(info_full + 8 * h);
+        const int s = warp - kCopyWarp - 1;
+        const float c = kLog2e / a.temperature, inv_t = 1.f / a.temperature;
+        RowInfo<T>& info = sm.info[s];
+        int32_t tok = 0;
+        float x_tok = NAN, w = 1.f, adv = 0.f, old = 0.f;
+        T edge = from_f32<T>(kNegInf);
+        // (a gradient in place comes later: it waits for this row's copy, which waits for this)
+        auto look = [&](int q) {
+            const int64_t i = group + (int64_t)q * groups;
+            if (OP == OP_DISTILL || q >= rows) return;
+            const Row<T> row(a, i);
+            tok = a.tokens ? a.tokens[i] : 0;
+            if (OP == OP_POLICY && lane == 0) {
+                w = a.weight ? a.weight[i] : 1.f;
+                adv = a.advantage[i];
+                old = a.old_logp ? a.old_logp[i] : 0.f;
             }
-        } else {
-            int32_t tok = 0;
-            float x_tok = NAN, w = 1.f, adv = 0.f, old = 0.f;
-            T edge = from_f32<T>(kNegInf);
-            auto look = [&](int64_t q) {  // (a gradient in place comes later: it waits for this row's copy, which waits for this)
-                if (q >= rows) return;
-                const int64_t i = group + q * groups;
-                const Row<T> row(a, i);
-                tok = a.tokens ? a.tokens[i] : 0;
-                if (lane == 0) {
-                    w = a.weight ? a.weight[i] : 1.f;
-                    if (OP == OP_POLICY) {
-                        adv = a.advantage[i];
-                        old = a.old_logp ? a.old_logp[i] : 0.f;
-                    }
-                }
-                x_tok = NAN;
-                if (tok >= 0) {
-                    edge = edge_element(row, first, plan.per_cta);
-                    if (lane == 0 && a.tokens && tok < row.vocab) x_tok = to_f32(row.x[tok]);
-                }
-            };
-            look(h);
-            for (int64_t q = h; q < rows; q += kHelpers) {
-                mbar_wait(info_empty + 8 * h, (q / kSlots & 1) ^ 1, &sm.dead);
-                RowInfo& info = sm.info[h];
-                keep_edge(info, edge);
-                if (lane == 0) {
+            x_tok = NAN;
+            if (tok >= 0) {
+                edge = edge_element(row, first, plan.per_cta);
+                if (lane == 0 && a.tokens && tok < row.vocab) x_tok = to_f32(row.x[tok]);
+            }
+        };
+        look(s);
+        for (int q = s; q < rows; q += kSlots) {
+            const int64_t i = group + (int64_t)q * groups;
+            const Row<T> row(a, i);
+            if (OP == OP_DISTILL) edge = edge_element(row, first, plan.per_cta);
+            mbar_wait(info_empty + 8 * s, parity_of(q) ^ 1, &sm.dead);
+            keep_edge(info, edge);
+            if constexpr (OP == OP_DISTILL)
+                teacher_ahead(a, i, row, first, max(0, min(plan.per_cta, row.n_vec - first)), rank, info, list_at(s), seen + s * kSeenWords);
+            if (lane == 0) {
+                info.row = row;
+                if (OP != OP_DISTILL) {
                     info.tok = tok;
                     info.live = tok >= 0;
                     info.x_tok = x_tok;
@@ -836,28 +866,107 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
                     info.adv = adv;
                     info.old = old;
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(info_full + 8 * h);
-                look(q + kHelpers);
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(info_full + 8 * s);
+            look(q + kSlots);
+
+            // ---- the row's results, from all parts in the same order
+            mbar_wait(parts_full + 8 * s, parity_of(q), &sm.dead);
+            Stats all;
+            float bound = kNegInf;
+            constexpr int kMost = (kMaxCluster * kWarps + 31) / 32;
+            float4 p[kMost];
+            const float4* parts = &sm.parts[s][0][0];
+#pragma unroll
+            for (int k = 0; k < kMost; ++k) {
+                p[k] = make_float4(kNegInf, 0.f, 0.f, INFINITY);
+                if (lane + 32 * k < cta_n * kWarps) p[k] = parts[lane + 32 * k];
+                all.m = fmaxf(all.m, p[k].x);
+            }
+            all.m = warp_max(all.m);
+#pragma unroll
+            for (int k = 0; k < kMost; ++k) {
+                const float d = p[k].x == kNegInf ? 0.f : c * (p[k].x - all.m), f = p[k].x == kNegInf ? 0.f : exp2_approx(d);
+                if (ENT) all.t += f * (p[k].z + p[k].y * fmaxf(d, -1e30f));
+                all.s += f * p[k].y;
+            }
+            all.s = warp_sum(all.s);
+            if (ENT) all.t = warp_sum(all.t);
+            if (*(volatile int*)&sm.dead) all.s = NAN;
+            if constexpr (TOP) {  // the least over this CTA's warps
+                bound = lane < kWarps ? sm.parts[s][rank][lane].w : INFINITY;
+#pragma unroll
+                for (int off = 16; off; off >>= 1) bound = fminf(bound, __shfl_xor_sync(0xffffffffu, bound, off));
+            }
+            const RowResult res(all, c, inv_t);
+            const bool live = info.live;
+            if constexpr (OP == OP_LOGPROBS) {
+                if (rank == 0 && lane == 0) {
+                    if (a.logp) a.logp[i] = !live ? 0.f : info.tok < row.vocab ? res.logp(info.x_tok) : NAN;
+                    if (a.entropy) a.entropy[i] = live ? res.entropy : 0.f;
+                    if (a.lse) a.lse[i] = live ? res.lse : 0.f;
+                }
+                if constexpr (TOP) {
+                    alternatives(a, i, sh, s, parity_of(q), rank, cta_n, bound, res, &sm.dead);
+                    __syncwarp();
+                    if (lane == 0) sh.n[s] = 0;
+                }
+            }
+            Coef f{};
+            if constexpr (OP == OP_POLICY) {
+                float g;
+                const float logp = info.tok < row.vocab ? res.logp(info.x_tok) : NAN;
+                const float term = policy_term(logp, info.adv, a.old_logp ? &info.old : nullptr, 0, a.clip_low, a.clip_high, g);
+                const float wt = info.w * inv_t;
+                f.k0 = wt * (ENT ? a.entropy_coef * res.entropy - g : -g);
+                f.k1 = ENT ? wt * a.entropy_coef * kLn2 : 0.f;
+                f.k2 = wt * g;
+                f.terms = info.tok < row.vocab && !res.empty;
+                if (rank == 0 && lane == 0) {
+                    a.loss[i] = !live ? 0.f : info.w * (ENT ? term - a.entropy_coef * res.entropy : term);
+                    if (a.logp) a.logp[i] = live ? logp : 0.f;
+                    if (ENT && a.entropy) a.entropy[i] = live ? res.entropy : 0.f;
+                }
+            }
+            if constexpr (OP == OP_DISTILL) {
+                f.k0 = info.bad ? NAN : info.w * inv_t;
+                f.terms = !info.bad && !isnan(res.lse) && !res.empty;
+            }
+            if (lane == 0) {
+                f.m = res.m;
+                f.log2_s = res.log2_s;
+                sm.coef[s] = f;
+                mbar_arrive(coef_full + 8 * s);
+            }
+            if (OP == OP_DISTILL && rank == 0) {
+                const TeacherList list = list_at(s);
+                float part = 0.f;
+                if (live && !info.bad)
+                    for (int k = lane; k < a.k; k += 32)
+                        if (list.id[k] >= 0) part += list.q[k] * (logf(list.q[k]) - res.logp(list.x[k]));
+                part = warp_sum(part);
+                if (lane == 0) a.loss[i] = !live ? 0.f : info.bad || isnan(res.lse) ? NAN : info.w * part;
+            }
+            __syncwarp();
         }
     } else if (warp == kCopyWarp) {
         // ---- the copies
         if (lane == 0) {
             int slot = 0, phase = 0;
-            for (int64_t q = 0; q < rows; ++q) {
-                const int s = q % kSlots;
-                mbar_wait(info_full + 8 * s, q / kSlots & 1, &sm.dead);
+            for (int q = 0; q < rows; ++q) {
+                const int s = slot_of(q);
+                mbar_wait(info_full + 8 * s, parity_of(q), &sm.dead);
                 const bool live = sm.info[s].live;
+                const Row<T> row = sm.info[s].row;
                 const uint4 head = sm.info[s].edge[0], tail = sm.info[s].edge[1];
                 mbar_arrive(info_empty + 8 * s);
                 if (!live) continue;
-                const Row<T> row(a, group + q * groups);
                 const int end = min(first + plan.per_cta, row.n_vec);
                 for (int v = first; v < end; v += plan.chunk) {
                     mbar_wait(empty + 8 * slot, phase ^ 1, &sm.dead);
                     const int last = min(v + plan.chunk, end) - 1;
-                    uint4* to = (uint4*)(ring + (size_t)slot * slot_bytes);
+                    uint4* to = (uint4*)(ring + slot * slot_bytes);
                     if (v == 0 && !row.whole(0)) to[0] = head;
                     if (last == row.n_vec - 1 && !row.whole(last) && last > 0) to[last - v] = tail;
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before a later copy to the same place
@@ -873,163 +982,108 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
                 }
             }
         }
-        __syncwarp();
     } else {
         // ---- the rows
-        const float c = kLog2e / a.temperature, inv_t = 1.f / a.temperature;
+        const float c = kLog2e / a.temperature;
         int slot_a = 0, phase_a = 0, slot_b = 0;  // the ring, at the row whose statistics are taken and at the one after
-        int64_t live_a = 0, live_b = 0;  // rows with statistics so far
-        float max_a = kNegInf, max_b = kNegInf;
-        auto slice_at = [&](const Row<T>& row, int slot) {
-            return Slice<T>{ring, slot, plan.chunks, slot_bytes, first, max(0, min(plan.per_cta, row.n_vec - first)), plan.chunk};
+        auto slice_at = [&](int n_vec, int slot) {
+            return Slice<T>{ring, slot, plan.chunks, slot_bytes, first, max(0, min(plan.per_cta, n_vec - first)), plan.chunk};
         };
 
-        auto statistics = [&](int64_t q) {
-            const int s = q % kSlots;
-            mbar_wait(info_full + 8 * s, q / kSlots & 1, &sm.dead);
-            if (!sm.info[s].live) return;
-            const Row<T> row(a, group + q * groups);
-            const Slice<T> slice = slice_at(row, slot_a);
+        auto statistics = [&](int q) {
+            const int s = slot_of(q);
+            mbar_wait(info_full + 8 * s, parity_of(q), &sm.dead);
             Running run;
-            slice.template each<4>(
-                [&](int slot) { mbar_wait(full + 8 * slot, phase_a, &sm.dead); },
-                [&](auto count, const uint4* r, int, bool) { run.add<T, ENT, decltype(count)::n>(r, c); },
-                [&](int slot) {
-                    if (!RES) {
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(empty + 8 * slot);
-                    }
-                    if (++slot_a == plan.chunks) slot_a = 0, phase_a ^= 1;
-                });
-            Stats st = run.stats();
             float bound = kNegInf;
-            max_a = st.m;
-            if constexpr (TOP) {  // this warp's ceil(k / kWarps)-th largest of its lanes' maxima
-                float v = st.m;
+            if (sm.info[s].live) {
+                const Slice<T> slice = slice_at(sm.info[s].row.n_vec, slot_a);
+                auto next = [&] { if (++slot_a == plan.chunks) slot_a = 0, phase_a ^= 1; };
+                if constexpr (TOP) {
+                    const int lead = sm.info[s].row.lead, need = (a.k + kWarps - 1) / kWarps - 1;
+                    Key* list = sh.list[s];
+                    float* bounds = sh.bound[q & 1];
+                    bool some = false;  // a bound is known
+                    slice.template each<4>(
+                        [&](int slot) { mbar_wait(full + 8 * slot, phase_a, &sm.dead); },
+                        [&](auto count, const uint4* r, int v, bool) {
+                            run.add<T, ENT, decltype(count)::n>(r, c);
+                            if (some) collect<T, decltype(count)::n>(r, v, lead, bound, list, &sh.n[s]);
+                        },
+                        [&](int slot, int k) {
+                            if ((k & (k + 1)) == 0) {  // after 1, 2, 4, ... chunks
+                                const float own = warp_kth(run.m, need);
+                                if (lane == 0) *(volatile float*)&bounds[warp] = own;
+                                if (k == 0)
+                                    row_threads_sync();
+                                else
+                                    __syncwarp();
+                                float b = lane < kWarps ? *(volatile float*)&bounds[lane] : INFINITY;
 #pragma unroll
-                for (int size = 2; size <= 32; size <<= 1)
-#pragma unroll
-                    for (int step = size >> 1; step; step >>= 1) {
-                        const float o = __shfl_xor_sync(0xffffffffu, v, step);
-                        const bool down = (lane & size) == 0, low = (lane & step) == 0;
-                        v = down == low ? fmaxf(v, o) : fminf(v, o);
+                                for (int off = 16; off; off >>= 1) b = fminf(b, __shfl_xor_sync(0xffffffffu, b, off));
+                                bound = b;
+                                some = true;
+                                if (k == 0)
+                                    slice.template chunk_of<1>(slot, 0, [&](Count<1>, const uint4* r, int v, bool) {
+                                        collect<T, 1>(r, v, lead, bound, list, &sh.n[s]);
+                                    });
+                            }
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(empty + 8 * slot);
+                            next();
+                        });
+                    row_threads_sync();
+                    if (sh.n[s] > kList) {
+                        row_threads_sync();
+                        collect_exact(sm.info[s].row, first, slice.n, a.k, sh, list, &sh.n[s]);
+                        bound = kNegInf;
+                    } else {
+                        bound = warp_kth(run.m, need);
                     }
-                bound = __shfl_sync(0xffffffffu, v, (a.k + kWarps - 1) / kWarps - 1);
+                } else {
+                    slice.template each<4>(
+                        [&](int slot) { mbar_wait(full + 8 * slot, phase_a, &sm.dead); },
+                        [&](auto count, const uint4* r, int, bool) { run.add<T, ENT, decltype(count)::n>(r, c); },
+                        [&](int slot, int) {
+                            if (!RES) {
+                                __syncwarp();
+                                if (lane == 0) mbar_arrive(empty + 8 * slot);
+                            }
+                            next();
+                        });
+                }
             }
+            Stats st = run.stats();
             st.join_warp<ENT>(c);
-            const int x = live_a++ % kSlots;
-            if (tid == 0) mbar_expect(parts_full + 8 * x, cta_n * kWarps * 16);
+            if (!RES && q >= 2) mbar_wait(coef_full + 8 * slot_of(q - 2), parity_of(q - 2), &sm.dead);  // (as RES does in rest)
+            if (tid == 0) mbar_expect(parts_full + 8 * s, cta_n * kWarps * 16);
             if (lane < cta_n)
-                send(map_to(smem_addr(&sm.parts[x][rank][warp]), lane), map_to(parts_full + 8 * x, lane), st.m, st.s, st.t, bound);
-        };
-
-        auto rest = [&](int64_t q) {
-            const int s = q % kSlots;
-            const int64_t i = group + q * groups;
-            const RowInfo& info = sm.info[s];
-            const Row<T> row(a, i);
-            const Slice<T> slice = slice_at(row, slot_b);
-            const bool tells = rank == 0 && tid == 0;  // writes the row's own results
-            if (!info.live) {
-                if constexpr (RES && OP != OP_LOGPROBS) {
-                    const uint4 zero = make_uint4(0, 0, 0, 0);
-                    for (int g = warp * 32; g < slice.n; g += kRowThreads) row.store(first + g + lane, zero, g + lane < slice.n);
-                }
-                if (tells) {
-                    if (a.logp) a.logp[i] = 0.f;
-                    if (a.entropy) a.entropy[i] = 0.f;
-                    if (a.lse) a.lse[i] = 0.f;
-                    if (a.loss) a.loss[i] = 0.f;
-                }
-                if (TOP && rank == 0)
-                    for (int k = tid; k < a.k; k += kRowThreads) {
-                        a.top_ids[i * a.k + k] = -1;
-                        a.top_logp[i * a.k + k] = kNegInf;
-                    }
+                send(map_to(smem_addr(&sm.parts[s][rank][warp]), lane), map_to(parts_full + 8 * s, lane), st.m, st.s, st.t, bound);
+            if (!RES) {
                 __syncwarp();
                 if (lane == 0) mbar_arrive(info_empty + 8 * s);
-                return;
             }
-            const int x = live_b % kSlots;
-            mbar_wait(parts_full + 8 * x, live_b / kSlots & 1, &sm.dead);
-            // every warp joins all parts, in the same order
-            Stats all;
-            float bound = kNegInf;
-            {
-                constexpr int kMost = (kMaxCluster * kWarps + 31) / 32;
-                float4 p[kMost];
-                const float4* parts = &sm.parts[x][0][0];
-#pragma unroll
-                for (int k = 0; k < kMost; ++k) {
-                    p[k] = make_float4(kNegInf, 0.f, 0.f, INFINITY);
-                    if (lane + 32 * k < cta_n * kWarps) p[k] = parts[lane + 32 * k];
-                    all.m = fmaxf(all.m, p[k].x);
-                }
-                all.m = warp_max(all.m);
-#pragma unroll
-                for (int k = 0; k < kMost; ++k) {
-                    const float d = p[k].x == kNegInf ? 0.f : c * (p[k].x - all.m), f = p[k].x == kNegInf ? 0.f : exp2_approx(d);
-                    if (ENT) all.t += f * (p[k].z + p[k].y * fmaxf(d, -1e30f));
-                    all.s += f * p[k].y;
-                    if constexpr (TOP) {  // the largest over the CTAs of the least over their warps
-                        float least = p[k].w;
-#pragma unroll
-                        for (int off = kWarps / 2; off; off >>= 1) least = fminf(least, __shfl_xor_sync(0xffffffffu, least, off));
-                        if (least < INFINITY) bound = fmaxf(bound, least);
-                    }
-                }
-                all.s = warp_sum(all.s);
-                if (ENT) all.t = warp_sum(all.t);
-                if constexpr (TOP)
-#pragma unroll
-                    for (int off = kWarps; off < 32; off <<= 1) bound = fmaxf(bound, __shfl_xor_sync(0xffffffffu, bound, off));
-            }
-            if (*(volatile int*)&sm.dead) all.s = NAN;
-            const RowResult res(all, c, inv_t);
-            const int32_t tok = info.tok;
+        };
 
-            float k0 = 0.f, k1 = 0.f, k2 = 0.f;  // the gradient p (k0 + k1 log2 p) + [j = token] k2
-            if constexpr (OP == OP_LOGPROBS) {
-                if (tells) {
-                    if (a.logp) a.logp[i] = tok < row.vocab ? res.logp(info.x_tok) : NAN;
-                    if (a.entropy) a.entropy[i] = res.entropy;
-                    if (a.lse) a.lse[i] = res.lse;
-                }
-            }
-            if constexpr (OP == OP_POLICY) {
-                float g;
-                const float logp = tok < row.vocab ? res.logp(info.x_tok) : NAN;
-                const float term = policy_term(logp, info.adv, a.old_logp ? &info.old : nullptr, 0, a.clip_low, a.clip_high, g);
-                if (tells) {
-                    a.loss[i] = info.w * (ENT ? term - a.entropy_coef * res.entropy : term);
-                    if (a.logp) a.logp[i] = logp;
-                    if (ENT && a.entropy) a.entropy[i] = res.entropy;
-                }
-                const float wt = info.w * inv_t;
-                k0 = wt * (ENT ? a.entropy_coef * res.entropy - g : -g);
-                k1 = ENT ? wt * a.entropy_coef * kLn2 : 0.f;
-                k2 = wt * g;
-            }
-            if constexpr (OP == OP_DISTILL) {
-                k0 = info.bad ? NAN : info.w * inv_t;
-                if (rank == 0 && warp == kWarps - 1) {
-                    const TeacherList list = list_at(s);
-                    float part = 0.f;
-                    if (!info.bad)
-                        for (int k = lane; k < a.k; k += 32)
-                            if (list.id[k] >= 0) part += list.q[k] * (logf(list.q[k]) - res.logp(list.x[k]));
-                    part = warp_sum(part);
-                    if (lane == 0) a.loss[i] = info.bad || isnan(res.lse) ? NAN : info.w * part;
-                }
-            }
-            if constexpr (RES && OP != OP_LOGPROBS) {
-                const F2 base(-res.m, -res.m), c2(c, c), less(-res.log2_s, -res.log2_s), k02(k0, k0), k12(k1, k1);
-                // ahead of the warp's first whole vector, and of the first after its last
+        auto rest = [&](int q) {
+            const int s = slot_of(q);
+            const RowInfo<T>& info = sm.info[s];
+            const Row<T> row = info.row;
+            const Slice<T> slice = slice_at(row.n_vec, slot_b);
+            mbar_wait(coef_full + 8 * s, parity_of(q), &sm.dead);
+            const Coef f = sm.coef[s];
+            if (!info.live) {
+                const uint4 zero = make_uint4(0, 0, 0, 0);
+                for (int g = warp * 32; g < slice.n; g += kRowThreads) row.store(first + g + lane, zero, g + lane < slice.n);
+            } else {
+                const F2 base(-f.m, -f.m), c2(c, c), less(-f.log2_s, -f.log2_s), k02(f.k0, f.k0), k12(f.k1, f.k1);
+                // a warp's vectors are all whole from plain_lo on and before plain_hi
                 const int plain_lo = row.whole_lo + lane, plain_hi = row.whole_lo + row.whole_n + lane - 31;
+                T* const dst0 = row.dx - row.lead;
                 slice.template each<2>(
                     [](int) {},
                     [&](auto count, const uint4* r, int v, bool act) {
                         constexpr int N = decltype(count)::n;
+                        static_assert(N <= 2);
                         uint4 out[N];
 #pragma unroll
                         for (int u = 0; u < N; ++u) {
@@ -1044,9 +1098,8 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
                             }
                             out[u] = Vec<T>::pack(y);
                         }
-                        T* dst = row.dx + ((int64_t)v * E - row.lead);
-                        static_assert(N <= 2);
                         if (row.shift == 0 && v >= plain_lo && v + (N - 1) * kRowThreads < plain_hi) {
+                            T* dst = dst0 + v * E;
 #pragma unroll
                             for (int u = 0; u < N; ++u)
                                 if (N > 1 || act) *(uint4*)(dst + u * kRowThreads * E) = out[u];
@@ -1055,64 +1108,54 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
                             for (int u = 0; u < N; ++u) row.store(v + u * kRowThreads, u == 0 ? out[0] : out[N - 1], act);
                         }
                     },
-                    [&](int slot) {
+                    [&](int slot, int) {
                         __syncwarp();
                         if (lane == 0) mbar_arrive(empty + 8 * slot);
+                        if (++slot_b == plan.chunks) slot_b = 0;
                     });
                 // the tokens that have a term of their own again, each by the warp that stored its vector
-                auto owner = [&](int id) { return ((id + row.lead) / E - first) % plan.chunk / 32 % kWarps; };
-                if constexpr (OP == OP_POLICY) {
-                    const int v = (tok + row.lead) / E - first;
-                    if (lane == 0 && tok < row.vocab && v >= 0 && v < slice.n && !res.empty && owner(tok) == warp) {
-                        const float d = fmaf(c, info.x_tok - res.m, -res.log2_s), p = exp2_approx(d);
-                        row.dx[tok] = from_f32<T>(fmaf(p, ENT ? fmaf(k1, fmaxf(d, -1e30f), k0) : k0, k2));
+                if (f.terms) {
+                    auto mine = [&](int id) {
+                        const int v = (id + row.lead) / E - first;
+                        return v >= 0 && v < slice.n && v % plan.chunk / 32 % kWarps == warp;
+                    };
+                    if constexpr (OP == OP_POLICY) {
+                        if (lane == 0 && mine(info.tok)) {
+                            const float d = fmaf(c, info.x_tok - f.m, -f.log2_s), p = exp2_approx(d);
+                            row.dx[info.tok] = from_f32<T>(fmaf(p, ENT ? fmaf(f.k1, fmaxf(d, -1e30f), f.k0) : f.k0, f.k2));
+                        }
                     }
-                }
-                if constexpr (OP == OP_DISTILL) {
-                    const TeacherList list = list_at(s);
-                    if (!info.bad && !isnan(res.lse) && !res.empty)
+                    if constexpr (OP == OP_DISTILL) {
+                        const TeacherList list = list_at(s);
                         for (int k = lane; k < info.n_own; k += 32) {
                             const int at = list.own[k], id = list.id[at];
-                            if (owner(id) != warp) continue;
+                            if (!mine(id)) continue;
                             float q = list.q[at];
                             if (info.repeats) {
                                 q = 0.f;
                                 for (int p = 0; p < info.n_own; ++p)
                                     if (list.id[list.own[p]] == id) q += list.q[list.own[p]];
                             }
-                            const float d = fmaf(c, list.x[at] - res.m, -res.log2_s);
-                            row.dx[id] = from_f32<T>((exp2_approx(d) - q) * k0);
+                            const float d = fmaf(c, list.x[at] - f.m, -f.log2_s);
+                            row.dx[id] = from_f32<T>((exp2_approx(d) - q) * f.k0);
                         }
+                    }
                 }
             }
-            if constexpr (TOP) {
-                const int turn = live_b / cta_n & 1;
-                const uint32_t to = live_b % cta_n;
-                if (rank == to && tid == 0) mbar_expect(smem_addr(&sh.full[turn]), cta_n * a.k * 8);
-                send_best(slice, row, a.k, max_b, isnan(res.lse) ? INFINITY : bound, sh, turn, rank, to);
-                slice.template each<1>([](int) {}, [](Count<1>, const uint4*, int, bool) {},
-                                       [&](int slot) { if (lane == 0) mbar_arrive(empty + 8 * slot); });
-                if (rank == to) {
-                    mbar_wait(smem_addr(&sh.full[turn]), live_b / (2 * cta_n) & 1, &sm.dead);
-                    merge_best(a, i, cta_n, res, sh, turn);
-                }
-            }
-            if (RES) slot_b = (slot_b + (slice.n + plan.chunk - 1) / plan.chunk) % plan.chunks;
-            ++live_b;
             __syncwarp();
             if (lane == 0) mbar_arrive(info_empty + 8 * s);
         };
 
-        if (plan.ahead) {
-            for (int64_t q = 0; q <= rows; ++q) {
-                max_b = max_a;
+        if constexpr (!RES) {
+            for (int q = 0; q < rows; ++q) statistics(q);
+        } else if (plan.ahead) {
+            for (int q = 0; q <= rows; ++q) {
                 if (q < rows) statistics(q);
                 if (q > 0) rest(q - 1);
             }
         } else {
-            for (int64_t q = 0; q < rows; ++q) {
+            for (int q = 0; q < rows; ++q) {
                 statistics(q);
-                max_b = max_a;
                 rest(q);
             }
         }
@@ -1196,11 +1239,12 @@ cudaError_t by_type(const RowArgs& a, F f) {
 constexpr int kSms = 152;
 constexpr int kMaxChunkVecs = 2048;
 
-template <typename T, int OP, bool RES, bool ENT>
+template <typename T, int OP, bool RES, bool ENT, bool TOP = false>
 cudaError_t launch_rows(const RowArgs& a, cudaStream_t s) {
     constexpr int E = Vec<T>::E;
-    constexpr int kMost = 232448 - (int)sizeof(RowShared) - (int)sizeof(typename OpShared<OP, RES>::type) - 1024;
-    const int lists = OP == OP_DISTILL ? kSlots * a.k * TeacherList::kBytes : 0, room = kMost - lists;
+    constexpr int kMost = 232448 - (int)sizeof(RowShared<T>) - 1024;
+    const int behind = TOP ? (int)sizeof(TopShared) : OP == OP_DISTILL ? kHelpers * kSeenWords * 4 + kSlots * a.k * TeacherList::kBytes : 0;
+    const int room = kMost - behind;
     // (rows that all begin in a line of their own have one vector less than rows at any place)
     const bool lines = (uintptr_t)a.x % 16 == 0 && (a.n == 1 || a.x_stride % E == 0);
     const int n_vec = (a.vocab + (lines ? 1 : 2) * (E - 1)) / E;
@@ -1218,7 +1262,7 @@ cudaError_t launch_rows(const RowArgs& a, cudaStream_t s) {
     const int own = (plan.per_cta + plan.chunk - 1) / plan.chunk;
     plan.ahead = !RES || 2 * own <= plan.chunks;
     if (RES && own > plan.chunks) return cudaErrorInvalidValue;
-    auto kernel = wide_kernel<T, OP, RES, ENT>;
+    auto kernel = wide_kernel<T, OP, RES, ENT, TOP>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
     if (e != cudaSuccess) return e;
     static const int kClusters[4] = {152, 76, 36, 15};  // of 1, 2, 4 and 8 CTAs that the GPU holds at once
@@ -1231,7 +1275,7 @@ cudaError_t launch_rows(const RowArgs& a, cudaStream_t s) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(clusters * plan.cta_n));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = (size_t)plan.chunks * plan.chunk * 16 + lists;
+    cfg.dynamicSmemBytes = (size_t)plan.chunks * plan.chunk * 16 + behind;
     cfg.stream = s;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
@@ -1251,7 +1295,7 @@ cudaError_t launch_back(const RowArgs& a, cudaStream_t s) {
 cudaError_t launch_token_logprobs(const RowArgs& a, cudaStream_t s) {
     return by_type(a, [&](auto t) {
         typedef decltype(t) T;
-        return a.k > 0 ? launch_rows<T, OP_LOGPROBS, true, true>(a, s) : launch_rows<T, OP_LOGPROBS, false, true>(a, s);
+        return a.k > 0 ? launch_rows<T, OP_LOGPROBS, false, true, true>(a, s) : launch_rows<T, OP_LOGPROBS, false, true>(a, s);
     });
 }
 
