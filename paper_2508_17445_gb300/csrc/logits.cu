@@ -8,15 +8,15 @@
 // would overflow in c x_j, and the row's largest terms lose nothing.
 //
 // All of it is bound by HBM: 8 to 20 operations an element against its 2 or 4
-// bytes, so a row is read once. wide_kernel is persistent: a cluster of CTAs takes
-// row after row, each CTA a slice of it, which bulk copies bring into a ring of
-// chunks in shared memory. Sixteen warps take the slice's statistics and send them
-// to every CTA of the cluster through distributed shared memory. A helper warp,
-// which had looked up the row's own values before its turn, joins them, writes the
-// row's results and leaves the gradient's coefficients, while the sixteen are at
-// the next row; then these make the gradient from the same chunks and give them
-// back to the ring. Nothing waits for a whole CTA. backward_kernel needs no
-// statistics and streams.
+// bytes. wide_kernel is persistent: a cluster of CTAs takes row after row, each CTA
+// a slice of it, which bulk copies bring chunk by chunk through a ring in shared
+// memory. Eight warps take the slice's statistics and send them to every CTA of the
+// cluster through distributed shared memory. A helper warp, which had looked up the
+// row's own values before its turn, joins them, writes the row's results and leaves
+// the gradient's coefficients; for the gradient the slice comes through the ring
+// once more, from L2, which holds the rows at work. So HBM reads a row once, the
+// whole ring is ahead of the work, and nothing waits for a whole CTA.
+// backward_kernel needs no statistics and streams.
 //
 // Rows start at any element: 16-byte vectors are counted from the line that the
 // row's logits begin in, and the two vectors at the ends that a row shares with
@@ -34,7 +34,7 @@ namespace tp {
 namespace {
 
 constexpr int kMaxCluster = 8;
-constexpr int kWarps = 16;           // that work on a row's elements
+constexpr int kWarps = 8;            // that work on a row's elements
 constexpr int kCopyWarp = kWarps;    // issues the bulk copies
 constexpr int kHelpers = 4;          // warps that look ahead at the rows' own values
 constexpr int kThreads = (kWarps + 1 + kHelpers) * 32;
@@ -64,6 +64,11 @@ struct F2 {
         get(a, b);
         return a + b;
     }
+    __device__ __forceinline__ F2 at_least(float x) const {
+        float a, b;
+        get(a, b);
+        return F2(fmaxf(a, x), fmaxf(b, x));
+    }
 };
 __device__ __forceinline__ F2 operator+(F2 a, F2 b) {
     F2 r;
@@ -79,6 +84,11 @@ __device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
     F2 r;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
     return r;
+}
+__device__ __forceinline__ F2 exp2_of(F2 x) {
+    float a, b;
+    x.get(a, b);
+    return F2(exp2_approx(a), exp2_approx(b));
 }
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -132,14 +142,35 @@ __device__ __forceinline__ uint64_t global_ns() {
 __device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
     if (mbar_try(bar, parity)) return;
     const uint64_t t0 = global_ns();
-    for (uint32_t i = 1; !*dead; ++i) {
+    for (uint32_t i = 1;; ++i) {
         if (mbar_try(bar, parity)) return;
-        if ((i & 63) == 0 && global_ns() - t0 > kWaitLimitNs) *dead = 1;
+        if ((i & 63) != 0) continue;
+        if (*dead) return;
+        if (global_ns() - t0 > kWaitLimitNs) *dead = 1;
     }
 }
-__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
-                 "r"(bytes), "r"(bar)
+// The same for a warp that looks ahead: it sleeps between looks and leaves the issue slots to the others.
+__device__ __forceinline__ void mbar_wait_idle(uint32_t bar, uint32_t parity, volatile int* dead) {
+    const uint64_t t0 = global_ns();
+    while (!mbar_try(bar, parity) && !*dead) {
+        __nanosleep(100);
+        if (global_ns() - t0 > kWaitLimitNs) *dead = 1;
+    }
+}
+// L2 keeps what is read again and lets go first of what is not.
+__device__ __forceinline__ uint64_t keep_in_l2() {
+    uint64_t p;
+    asm("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+__device__ __forceinline__ uint64_t pass_l2() {
+    uint64_t p;
+    asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar, uint64_t policy) {
+    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(dst),
+                 "l"(src), "r"(bytes), "r"(bar), "l"(policy)
                  : "memory");
 }
 __device__ __forceinline__ void row_threads_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kRowThreads) : "memory"); }
@@ -171,8 +202,20 @@ struct Vec<float> {
     static __device__ __forceinline__ uint4 pack(const float* v) {
         return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
     }
-    static __device__ __forceinline__ float max_of(const uint4& r) {  // NaN left out
-        return fmaxf(fmaxf(__uint_as_float(r.x), __uint_as_float(r.y)), fmaxf(__uint_as_float(r.z), __uint_as_float(r.w)));
+    template <int N>
+    static __device__ __forceinline__ float max_of(const uint4* r) {  // NaN left out
+        float m = kNegInf;
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+            m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(r[u].x), __uint_as_float(r[u].y)),
+                               fmaxf(__uint_as_float(r[u].z), __uint_as_float(r[u].w))));
+        return m;
+    }
+    // x - m of every element
+    static __device__ __forceinline__ void minus(const uint4& r, float m, F2* d) {
+        const F2 b(-m, -m);
+        d[0] = F2(__uint_as_float(r.x), __uint_as_float(r.y)) + b;
+        d[1] = F2(__uint_as_float(r.z), __uint_as_float(r.w)) + b;
     }
 };
 template <>
@@ -196,11 +239,25 @@ struct Vec<__nv_bfloat16> {
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
-    static __device__ __forceinline__ float max_of(const uint4& r) {
-        const __nv_bfloat162 *a = (const __nv_bfloat162*)&r.x, *b = (const __nv_bfloat162*)&r.y,
-                             *c = (const __nv_bfloat162*)&r.z, *d = (const __nv_bfloat162*)&r.w;
-        const float2 f = __bfloat1622float2(__hmax2(__hmax2(*a, *b), __hmax2(*c, *d)));
+    template <int N>
+    static __device__ __forceinline__ float max_of(const uint4* r) {
+        const __nv_bfloat162* h = (const __nv_bfloat162*)r;
+        __nv_bfloat162 m = h[0];
+#pragma unroll
+        for (int k = 1; k < 4 * N; ++k) m = __hmax2(m, h[k]);
+        const float2 f = __bfloat1622float2(m);
         return fmaxf(f.x, f.y);
+    }
+    static __device__ __forceinline__ void minus(const uint4& r, float m, F2* d) {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float a, b;
+            asm("{ .reg .b16 l, h; mov.b32 {l, h}, %2; sub.rn.f32.bf16 %0, l, %3; sub.rn.f32.bf16 %1, h, %3; }"
+                : "=f"(a), "=f"(b)
+                : "r"(w[k]), "f"(m));
+            d[k] = F2(a, b);
+        }
     }
 };
 template <>
@@ -225,10 +282,25 @@ struct Vec<__half> {
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
-    static __device__ __forceinline__ float max_of(const uint4& r) {
-        const __half2 *a = (const __half2*)&r.x, *b = (const __half2*)&r.y, *c = (const __half2*)&r.z, *d = (const __half2*)&r.w;
-        const float2 f = __half22float2(__hmax2(__hmax2(*a, *b), __hmax2(*c, *d)));
+    template <int N>
+    static __device__ __forceinline__ float max_of(const uint4* r) {
+        const __half2* h = (const __half2*)r;
+        __half2 m = h[0];
+#pragma unroll
+        for (int k = 1; k < 4 * N; ++k) m = __hmax2(m, h[k]);
+        const float2 f = __half22float2(m);
         return fmaxf(f.x, f.y);
+    }
+    static __device__ __forceinline__ void minus(const uint4& r, float m, F2* d) {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float a, b;
+            asm("{ .reg .b16 l, h; mov.b32 {l, h}, %2; sub.rn.f32.f16 %0, l, %3; sub.rn.f32.f16 %1, h, %3; }"
+                : "=f"(a), "=f"(b)
+                : "r"(w[k]), "f"(m));
+            d[k] = F2(a, b);
+        }
     }
 };
 
@@ -334,39 +406,60 @@ struct Stats {
     }
 };
 
-// A thread's, as it goes; even and odd elements apart.
+// A thread's, as it goes; even and odd elements apart. p d of a logit of -inf (or
+// so low that d overflows) is 0 times -inf: the vectors whose sum of them is NaN
+// for that reason are summed again, and `low` remembers that the row has such.
 struct Running {
-    float m = kNegInf;
-    F2 base{0.f, 0.f};  // -m, or 0 while there is none
+    float m = kNegInf, base = 0.f;  // base: m, or 0 while there is none
     F2 s{0.f, 0.f}, t{0.f, 0.f};
+    bool low = false;
 
     __device__ __forceinline__ void raise(float m2, float c) {  // m2 > m
         const float d = m == kNegInf ? 0.f : fmaxf(c * (m - m2), -1e30f), f = m == kNegInf ? 0.f : exp2_approx(d);
         const F2 d2(d, d), f2(f, f);
         t = f2 * fma2(s, d2, t);
         s = f2 * s;
-        m = m2;
-        base = F2(-m2, -m2);
+        m = base = m2;
     }
     template <typename T, bool ENT, int N>
     __device__ __forceinline__ void add(const uint4* r, float c) {
-        float m2 = Vec<T>::max_of(r[0]);
-#pragma unroll
-        for (int u = 1; u < N; ++u) m2 = fmaxf(m2, Vec<T>::max_of(r[u]));
+        const float m2 = Vec<T>::template max_of<N>(r);
         if (m2 > m) raise(m2, c);
         const F2 c2(c, c);
+        F2 part(0.f, 0.f);
 #pragma unroll
         for (int u = 0; u < N; ++u) {
-            float x[Vec<T>::E];
-            Vec<T>::unpack(r[u], x);
+            F2 d[Vec<T>::E / 2];
+            Vec<T>::minus(r[u], base, d);
 #pragma unroll
-            for (int e = 0; e < Vec<T>::E; e += 2) {
-                float d0, d1;
-                ((F2(x[e], x[e + 1]) + base) * c2).get(d0, d1);
-                const F2 p(exp2_approx(d0), exp2_approx(d1));
+            for (int e = 0; e < Vec<T>::E / 2; ++e) {
+                d[e] = d[e] * c2;
+                const F2 p = exp2_of(d[e]);
                 s = s + p;
-                if (ENT) t = fma2(p, F2(fmaxf(d0, -1e30f), fmaxf(d1, -1e30f)), t);  // (0 times -inf stays 0)
+                if (ENT) part = fma2(p, d[e], part);
             }
+        }
+        if (ENT) {
+            const float sum = part.sum();
+            if (sum != sum) {
+                low = true;
+                part = F2(0.f, 0.f);
+#pragma unroll 1
+                for (int u = 0; u < N; ++u) {
+                    uint4 v = r[0];
+#pragma unroll
+                    for (int w = 1; w < N; ++w)
+                        if (u == w) v = r[w];
+                    F2 d[Vec<T>::E / 2];
+                    Vec<T>::minus(v, base, d);
+#pragma unroll
+                    for (int e = 0; e < Vec<T>::E / 2; ++e) {
+                        d[e] = (d[e] * c2);
+                        part = fma2(exp2_of(d[e]), d[e].at_least(-1e30f), part);
+                    }
+                }
+            }
+            t = t + part;
         }
     }
     __device__ __forceinline__ Stats stats() const {
@@ -428,6 +521,7 @@ struct RowInfo {
 struct Coef {
     float m, log2_s, k0, k1, k2;
     int32_t terms;  // whether tokens have terms of their own
+    int32_t low;    // whether log2 p may be infinite where p = 0
 };
 
 template <typename T>
@@ -456,72 +550,77 @@ constexpr int kSeenWords = 256;  // a bit for the tokens of equal residue, by wh
 
 // Alternatives. A key holds a logit, in an order of unsigned integers, above the
 // complement of its id: the k largest keys are the k largest logits, of equal ones
-// the lower ids. Where each of a CTA's warps has ceil(k / kWarps) lanes that have
-// met a logit of at least b, nothing below b is among the slice's k. The warps
-// take that b from their lanes' maxima after the first chunk and again after 2, 4,
-// 8, ...; what is not below it goes on the row's list. The helper warp leaves out
-// what the last bound excludes, ranks the rest by comparing all with all, and one
-// CTA's helper merges the cluster's. A list that overflows (many equal logits, or
-// rows in rising order) is made again by finding the k-th largest key by digits.
-constexpr int kList = 1024;
+// the lower ids. Where k threads have met a logit of at least b, nothing below b is
+// among the slice's k. After the first chunk each warp takes the ceil(k / kWarps)-th
+// of its lanes' maxima and the CTA the least of these; from then on the threads
+// leave their maxima after every chunk, and the row's helper warp makes a higher b
+// of them as often as it can. What is not below b goes on the row's list. In the
+// end the helper leaves out what the last b excludes and ranks the rest by comparing
+// all with all, and one CTA's helper merges the cluster's. A list that overflows
+// (many equal logits, rows in rising order) is made again by finding the k-th
+// largest key by its digits.
 struct TopShared {
-    Key list[kSlots][kList];
-    Key best[kSlots][kMaxCluster][TP_MAX_ALTERNATIVES];  // the first CTA's: each CTA's keys, descending, 0 where none is left
     uint64_t best_full[kSlots];
-    float bound[2][kWarps];
+    float most[kSlots][kRowThreads];  // the threads' largest logits so far
+    float bound[kSlots];              // what the helper has made of them
+    float first[2][kWarps];
     int n[kSlots];
     int digit, rest;
     int hist[256];
+    // behind it: the slots' lists of list_size(k) keys, then the first CTA's best keys of each slot and CTA: k, descending,
+    // 0 where none is left
+
+    static __host__ __device__ __forceinline__ int list_size(int k) { return 1024 + 8 * k; }
+    static __host__ __forceinline__ int bytes(int k, int cta_n) {
+        return (int)sizeof(TopShared) + kSlots * 8 * (list_size(k) + (cta_n > 1 ? cta_n * k : 0));
+    }
+    __device__ __forceinline__ Key* list(int s, int k) { return (Key*)(this + 1) + s * list_size(k); }
+    __device__ __forceinline__ Key* best(int s, int rank, int k, int cta_n) {
+        return (Key*)(this + 1) + kSlots * list_size(k) + (s * cta_n + rank) * k;
+    }
 };
+
 struct Plan {
     int cta_n;          // CTAs a cluster
     int chunk, chunks;  // vectors a chunk, chunks of the ring
     int per_cta;        // vectors a slice
-    int ahead;          // whether a row's statistics are begun before the last row is done
 };
 
-// One row's chunks in the ring, as the working warps see them: groups of 32
-// vectors, group g of a chunk is warp (g % kWarps)'s.
+// A row's slice as the working warps see it: groups of 32 vectors, group g of a
+// chunk is warp (g % kWarps)'s.
 template <int N>
 struct Count {
     static constexpr int n = N;
 };
 template <typename T>
 struct Slice {
-    const uint8_t* ring;
-    int slot, slots, slot_bytes;  // the first chunk's
-    int first, n, chunk;          // the slice's first vector, its vectors, a chunk's
+    int first, n, chunk;  // the slice's first vector, its vectors, a chunk's
 
-    // f(Count<M>, vectors read (M, kRowThreads apart), the first's number in the row, act) with M = N or 1,
-    // over the chunk that begins at vector v0 of the slice.
+    __device__ __forceinline__ int chunks() const { return (n + chunk - 1) / chunk; }
+    // f(Count<M>, vectors read (M, kRowThreads apart), the first's number in the row, act) with M = N, 2 or 1,
+    // over chunk k, which lies at `at`.
     template <int N, typename F>
-    __device__ __forceinline__ void chunk_of(int at, int v0, F f) const {
+    __device__ __forceinline__ void each(const uint8_t* at, int k, F f) const {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-        const uint4* data = (const uint4*)(ring + at * slot_bytes) + lane;
-        const int m = min(chunk, n - v0), v = first + v0 + lane;
+        const uint4* data = (const uint4*)at + lane;
+        const int m = min(chunk, n - k * chunk), v = first + k * chunk + lane;
         int g = warp * 32;
-        for (; g + (N - 1) * kRowThreads + 32 <= m; g += N * kRowThreads) {
-            uint4 r[N];
+        auto some = [&](auto count) {
+            constexpr int M = decltype(count)::n;
+            uint4 r[M];
 #pragma unroll
-            for (int u = 0; u < N; ++u) r[u] = data[g + u * kRowThreads];
-            f(Count<N>{}, r, v + g, true);
-        }
+            for (int u = 0; u < M; ++u) r[u] = data[g + u * kRowThreads];
+            f(count, r, v + g, true);
+            g += M * kRowThreads;
+        };
+        while (g + (N - 1) * kRowThreads + 32 <= m) some(Count<N>{});
+        if constexpr (N > 2)
+            if (g + kRowThreads + 32 <= m) some(Count<2>{});
         for (; g < m; g += kRowThreads) {
             uint4 r = make_uint4(Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone);
             const bool act = g + lane < m;
             if (act) r = data[g];
             f(Count<1>{}, &r, v + g, act);
-        }
-    }
-    // The same over the slice; wait(slot) before a chunk, done(slot, its number) after it.
-    template <int N, typename W, typename F, typename D>
-    __device__ __forceinline__ void each(W wait, F f, D done) const {
-        int at = slot;
-        for (int v0 = 0, k = 0; v0 < n; v0 += chunk, ++k) {
-            wait(at);
-            chunk_of<N>(at, v0, f);
-            done(at, k);
-            if (++at == slots) at = 0;
         }
     }
 };
@@ -553,18 +652,18 @@ __device__ __forceinline__ float warp_kth(float v, int at) {
 
 // Puts the logits of M vectors that are not below the bound on the list.
 template <typename T, int M>
-__device__ __forceinline__ void collect(const uint4* r, int v, int lead, float bound, Key* list, int* n) {
+__device__ __forceinline__ void collect(const uint4* r, int v, int lead, float bound, Key* list, int size, int* n) {
     constexpr int E = Vec<T>::E;
 #pragma unroll
     for (int u = 0; u < M; ++u)
-        if (Vec<T>::max_of(r[u]) >= bound) {
+        if (Vec<T>::template max_of<1>(r + u) >= bound) {
             float x[E];
             Vec<T>::unpack(r[u], x);
 #pragma unroll
             for (int e = 0; e < E; ++e)
                 if (x[e] >= bound && x[e] > kNegInf) {
                     const int at = atomicAdd(n, 1);
-                    if (at < kList) list[at] = make_key(x[e], (v + u * kRowThreads) * E + e - lead);
+                    if (at < size) list[at] = make_key(x[e], (v + u * kRowThreads) * E + e - lead);
                 }
         }
 }
@@ -629,18 +728,46 @@ __device__ __noinline__ void collect_exact(const Row<T>& row, int first, int n, 
     each_key([&](Key key) {
         if (key >= found) {
             const int at = atomicAdd(count, 1);
-            if (at < kList) list[at] = key;  // (k of them)
+            list[at] = key;  // (k of them)
         }
     });
     row_threads_sync();
 }
 
-// One helper warp: the row's alternatives from the CTAs' lists. bound: the slice's last.
+// One helper warp: a value, at least b, that k of the threads' maxima are not below (b or -inf where there are fewer).
+// Halving between the largest and b, in the order of keys, until at most k / 8 too many are left.
+__device__ __forceinline__ float kth_of_maxima(const float* most, int k, float b) {
+    const int lane = threadIdx.x & 31;
+    uint32_t v[kRowThreads / 32], lo = (uint32_t)(make_key(b, 0) >> 32), hi = lo;
+#pragma unroll
+    for (int j = 0; j < kRowThreads / 32; ++j) {
+        v[j] = (uint32_t)(make_key(((volatile const float*)most)[lane + 32 * j], 0) >> 32);
+        hi = max(hi, v[j]);
+    }
+    hi = __reduce_max_sync(0xffffffffu, hi) + 1;
+    while (hi - lo > 1) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        uint32_t n = 0;
+#pragma unroll
+        for (int j = 0; j < kRowThreads / 32; ++j) n += v[j] >= mid;
+        n = __reduce_add_sync(0xffffffffu, n);
+        if ((int)n < k) {
+            hi = mid;
+            continue;
+        }
+        lo = mid;
+        if ((int)n <= k + k / 8) break;
+    }
+    return key_value((Key)lo << 32);
+}
+
+// One helper warp: the row's alternatives from the CTAs' lists. bound: nothing below it is one of them.
 __device__ __forceinline__ void alternatives(const RowArgs& a, int64_t i, TopShared& sh, int s, uint32_t parity, uint32_t rank, int cta_n,
                                              float bound, const RowResult& r, volatile int* dead) {
     const int lane = threadIdx.x & 31, k = a.k;
-    Key* list = sh.list[s];
-    const int met = min(sh.n[s], kList);
+    Key* list = sh.list(s, k);
+    const int met = min(sh.n[s], TopShared::list_size(k));
+    if (met > 2 * k + 32) bound = fmaxf(bound, kth_of_maxima(sh.most[s], k, bound));
     const Key least = bound > kNegInf ? make_key(bound, 0x7fffffff) : 0;  // of its equals the last
     int m = 0;
     for (int p0 = 0; p0 < met; p0 += 32) {  // left out in place: never written ahead of what is read
@@ -656,13 +783,14 @@ __device__ __forceinline__ void alternatives(const RowArgs& a, int64_t i, TopSha
         a.top_ids[i * k + place] = some ? key_id(key) : -1;
         a.top_logp[i * k + place] = nan ? NAN : some ? r.logp(key_value(key)) : kNegInf;
     };
-    const uint32_t bar = map_to(smem_addr(&sh.best_full[s]), 0), dst = map_to(smem_addr(&sh.best[s][rank][0]), 0);
+    const uint32_t bar = map_to(smem_addr(&sh.best_full[s]), 0), dst = map_to(smem_addr(sh.best(s, rank, k, cta_n)), 0);
     if (!alone && rank == 0 && lane == 0) mbar_expect(smem_addr(&sh.best_full[s]), cta_n * k * 8);
     for (int p = lane; p < max(m, k); p += 32) {
         const Key key = p < m ? list[p] : 0;
         int place = p;
         if (p < m) {
             place = 0;
+#pragma unroll 8
             for (int q = 0; q < m; ++q) place += list[q] > key;
         }
         if (place >= k) continue;
@@ -673,23 +801,26 @@ __device__ __forceinline__ void alternatives(const RowArgs& a, int64_t i, TopSha
     }
     if (alone || rank != 0) return;
     mbar_wait(smem_addr(&sh.best_full[s]), parity, dead);
+    const Key* best = sh.best(s, 0, k, cta_n);
+    int top = 1;
+    while (2 * top <= k) top *= 2;
     for (int p = lane; p < cta_n * k; p += 32) {
-        const int own = p / k, at = p - own * k;
-        const Key key = sh.best[s][own][at];
-        int place = at;
-        for (int q = 0; q < cta_n && place < k; ++q) {
-            if (q == own) continue;
-            int lo = 0, hi = k;  // how many of q's come before: larger, or for "none" (0) the lower CTA's
-            while (lo < hi) {
-                const int mid = (lo + hi) / 2;
-                const Key o = sh.best[s][q][mid];
-                if (o > key || (o == key && q < own))
-                    lo = mid + 1;
-                else
-                    hi = mid;
+        const int own = p / k;
+        const Key key = best[p];
+        // how many of each CTA's come before: larger, or for "none" (0) the lower CTA's; the searches side by side
+        int before[kMaxCluster] = {};
+        for (int step = top; step; step /= 2)
+#pragma unroll
+            for (int q = 0; q < kMaxCluster; ++q) {
+                const int at = before[q] + step;
+                if (q >= cta_n || at > k) continue;
+                const Key o = best[q * k + at - 1];
+                if (o > key || (o == key && q < own)) before[q] = at;
             }
-            place += lo;
-        }
+        int place = p - own * k;
+#pragma unroll
+        for (int q = 0; q < kMaxCluster; ++q)
+            if (q != own) place += before[q];
         if (place < k) write(place, key);
     }
 }
@@ -772,10 +903,9 @@ __device__ __forceinline__ void teacher_ahead(const RowArgs& a, int64_t i, const
     }
 }
 
-// RES: the slice stays in the ring until the row's statistics are known, for a
-// gradient. ENT: the entropy is asked for (or in the gradient). TOP: alternatives.
-template <typename T, int OP, bool RES, bool ENT, bool TOP>
-__global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant__ RowArgs a, const __grid_constant__ Plan plan) {
+// GRAD: a gradient is asked for. ENT: the entropy is (or is in the gradient). TOP: alternatives.
+template <typename T, int OP, bool GRAD, bool ENT, bool TOP>
+__global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant__ RowArgs a, const __grid_constant__ Plan plan) {
     extern __shared__ __align__(128) uint8_t ring[];
     __shared__ RowShared<T> sm;
     constexpr int E = Vec<T>::E;
@@ -809,7 +939,6 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             mbar_init(coef_full + 8 * k, 1);
             if constexpr (TOP) {
                 mbar_init(smem_addr(&sh.best_full[k]), 1);
-                sh.n[k] = 0;
             }
         }
         sm.dead = 0;
@@ -852,7 +981,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             const int64_t i = group + (int64_t)q * groups;
             const Row<T> row(a, i);
             if (OP == OP_DISTILL) edge = edge_element(row, first, plan.per_cta);
-            mbar_wait(info_empty + 8 * s, parity_of(q) ^ 1, &sm.dead);
+            mbar_wait_idle(info_empty + 8 * s, parity_of(q) ^ 1, &sm.dead);
             keep_edge(info, edge);
             if constexpr (OP == OP_DISTILL)
                 teacher_ahead(a, i, row, first, max(0, min(plan.per_cta, row.n_vec - first)), rank, info, list_at(s), seen + s * kSeenWords);
@@ -867,22 +996,36 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
                     info.old = old;
                 }
             }
+            if constexpr (TOP) {
+                for (int k = lane; k < kRowThreads; k += 32) sh.most[s][k] = kNegInf;
+                if (lane == 0) sh.bound[s] = kNegInf, sh.n[s] = 0;
+            }
             __syncwarp();
             if (lane == 0) mbar_arrive(info_full + 8 * s);
             look(q + kSlots);
+            if constexpr (TOP) {
+                float b = kNegInf;
+                while (plan.per_cta > plan.chunk && !mbar_try(parts_full + 8 * s, parity_of(q)) && !*(volatile int*)&sm.dead) {
+                    b = kth_of_maxima(sh.most[s], a.k, b);
+                    if (lane == 0) *(volatile float*)&sh.bound[s] = b;
+                    __syncwarp();
+                }
+            }
 
             // ---- the row's results, from all parts in the same order
-            mbar_wait(parts_full + 8 * s, parity_of(q), &sm.dead);
+            mbar_wait_idle(parts_full + 8 * s, parity_of(q), &sm.dead);
             Stats all;
             float bound = kNegInf;
+            bool low = false;
             constexpr int kMost = (kMaxCluster * kWarps + 31) / 32;
             float4 p[kMost];
             const float4* parts = &sm.parts[s][0][0];
 #pragma unroll
             for (int k = 0; k < kMost; ++k) {
-                p[k] = make_float4(kNegInf, 0.f, 0.f, INFINITY);
+                p[k] = make_float4(kNegInf, 0.f, 0.f, TOP ? kNegInf : 0.f);
                 if (lane + 32 * k < cta_n * kWarps) p[k] = parts[lane + 32 * k];
                 all.m = fmaxf(all.m, p[k].x);
+                low |= p[k].w != 0.f;
             }
             all.m = warp_max(all.m);
 #pragma unroll
@@ -894,40 +1037,27 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             all.s = warp_sum(all.s);
             if (ENT) all.t = warp_sum(all.t);
             if (*(volatile int*)&sm.dead) all.s = NAN;
-            if constexpr (TOP) {  // the least over this CTA's warps
-                bound = lane < kWarps ? sm.parts[s][rank][lane].w : INFINITY;
+            if constexpr (TOP) {  // the largest of the CTAs' bounds (none: -inf, their lists are exact)
+                bound = kNegInf;
 #pragma unroll
-                for (int off = 16; off; off >>= 1) bound = fminf(bound, __shfl_xor_sync(0xffffffffu, bound, off));
+                for (int k = 0; k < kMost; ++k)
+                    if (p[k].w < INFINITY) bound = fmaxf(bound, p[k].w);
+                bound = warp_max(bound);
             }
             const RowResult res(all, c, inv_t);
             const bool live = info.live;
-            if constexpr (OP == OP_LOGPROBS) {
-                if (rank == 0 && lane == 0) {
-                    if (a.logp) a.logp[i] = !live ? 0.f : info.tok < row.vocab ? res.logp(info.x_tok) : NAN;
-                    if (a.entropy) a.entropy[i] = live ? res.entropy : 0.f;
-                    if (a.lse) a.lse[i] = live ? res.lse : 0.f;
-                }
-                if constexpr (TOP) {
-                    alternatives(a, i, sh, s, parity_of(q), rank, cta_n, bound, res, &sm.dead);
-                    __syncwarp();
-                    if (lane == 0) sh.n[s] = 0;
-                }
-            }
             Coef f{};
+            float logp = NAN, term = 0.f;
+            if (OP != OP_DISTILL && info.tok < row.vocab) logp = res.logp(info.x_tok);
             if constexpr (OP == OP_POLICY) {
                 float g;
-                const float logp = info.tok < row.vocab ? res.logp(info.x_tok) : NAN;
-                const float term = policy_term(logp, info.adv, a.old_logp ? &info.old : nullptr, 0, a.clip_low, a.clip_high, g);
+                term = policy_term(logp, info.adv, a.old_logp ? &info.old : nullptr, 0, a.clip_low, a.clip_high, g);
                 const float wt = info.w * inv_t;
                 f.k0 = wt * (ENT ? a.entropy_coef * res.entropy - g : -g);
                 f.k1 = ENT ? wt * a.entropy_coef * kLn2 : 0.f;
                 f.k2 = wt * g;
+                f.low = __any_sync(0xffffffffu, low);
                 f.terms = info.tok < row.vocab && !res.empty;
-                if (rank == 0 && lane == 0) {
-                    a.loss[i] = !live ? 0.f : info.w * (ENT ? term - a.entropy_coef * res.entropy : term);
-                    if (a.logp) a.logp[i] = live ? logp : 0.f;
-                    if (ENT && a.entropy) a.entropy[i] = live ? res.entropy : 0.f;
-                }
             }
             if constexpr (OP == OP_DISTILL) {
                 f.k0 = info.bad ? NAN : info.w * inv_t;
@@ -939,6 +1069,13 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
                 sm.coef[s] = f;
                 mbar_arrive(coef_full + 8 * s);
             }
+            if (rank == 0 && lane == 0 && OP != OP_DISTILL) {
+                if (OP == OP_POLICY) a.loss[i] = !live ? 0.f : info.w * (ENT ? term - a.entropy_coef * res.entropy : term);
+                if (a.logp) a.logp[i] = live ? logp : 0.f;
+                if (ENT && a.entropy) a.entropy[i] = live ? res.entropy : 0.f;
+                if (OP == OP_LOGPROBS && a.lse) a.lse[i] = live ? res.lse : 0.f;
+            }
+            if constexpr (TOP) alternatives(a, i, sh, s, parity_of(q), rank, cta_n, bound, res, &sm.dead);
             if (OP == OP_DISTILL && rank == 0) {
                 const TeacherList list = list_at(s);
                 float part = 0.f;
@@ -963,102 +1100,100 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
                 mbar_arrive(info_empty + 8 * s);
                 if (!live) continue;
                 const int end = min(first + plan.per_cta, row.n_vec);
-                for (int v = first; v < end; v += plan.chunk) {
-                    mbar_wait(empty + 8 * slot, phase ^ 1, &sm.dead);
-                    const int last = min(v + plan.chunk, end) - 1;
-                    uint4* to = (uint4*)(ring + slot * slot_bytes);
-                    if (v == 0 && !row.whole(0)) to[0] = head;
-                    if (last == row.n_vec - 1 && !row.whole(last) && last > 0) to[last - v] = tail;
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before a later copy to the same place
-                    const int v0 = max(v, row.whole_lo), v1 = min(min(v + plan.chunk, end), row.whole_lo + row.whole_n);
-                    if (v1 > v0 && !*(volatile int*)&sm.dead) {
-                        mbar_expect(full + 8 * slot, (v1 - v0) * 16);
-                        bulk_copy(smem_addr(ring) + slot * slot_bytes + (v0 - v) * 16, row.x + ((int64_t)v0 * E - row.lead),
-                                  (v1 - v0) * 16, full + 8 * slot);
-                    } else {
-                        mbar_arrive(full + 8 * slot);
+                for (int pass = 0; pass < (GRAD ? 2 : 1); ++pass)
+                    for (int v = first; v < end; v += plan.chunk) {
+                        mbar_wait(empty + 8 * slot, phase ^ 1, &sm.dead);
+                        const int last = min(v + plan.chunk, end) - 1;
+                        uint4* to = (uint4*)(ring + slot * slot_bytes);
+                        if (v == 0 && !row.whole(0)) to[0] = head;
+                        if (last == row.n_vec - 1 && !row.whole(last) && last > 0) to[last - v] = tail;
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before a later copy to the same place
+                        const int v0 = max(v, row.whole_lo), v1 = min(min(v + plan.chunk, end), row.whole_lo + row.whole_n);
+                        if (v1 > v0 && !*(volatile int*)&sm.dead) {
+                            mbar_expect(full + 8 * slot, (v1 - v0) * 16);
+                            bulk_copy(smem_addr(ring) + slot * slot_bytes + (v0 - v) * 16, row.x + ((int64_t)v0 * E - row.lead),
+                                      (v1 - v0) * 16, full + 8 * slot, GRAD && pass == 0 ? keep_in_l2() : pass_l2());
+                        } else {
+                            mbar_arrive(full + 8 * slot);
+                        }
+                        if (++slot == plan.chunks) slot = 0, phase ^= 1;
                     }
-                    if (++slot == plan.chunks) slot = 0, phase ^= 1;
-                }
             }
         }
     } else {
         // ---- the rows
         const float c = kLog2e / a.temperature;
-        int slot_a = 0, phase_a = 0, slot_b = 0;  // the ring, at the row whose statistics are taken and at the one after
-        auto slice_at = [&](int n_vec, int slot) {
-            return Slice<T>{ring, slot, plan.chunks, slot_bytes, first, max(0, min(plan.per_cta, n_vec - first)), plan.chunk};
+        int at_slot = 0, at_phase = 0;  // of the ring
+        auto chunk_here = [&] {
+            mbar_wait(full + 8 * at_slot, at_phase, &sm.dead);
+            return (const uint8_t*)ring + at_slot * slot_bytes;
         };
+        auto chunk_done = [&] {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(empty + 8 * at_slot);
+            if (++at_slot == plan.chunks) at_slot = 0, at_phase ^= 1;
+        };
+        auto slice_at = [&](int n_vec) { return Slice<T>{first, max(0, min(plan.per_cta, n_vec - first)), plan.chunk}; };
 
         auto statistics = [&](int q) {
             const int s = slot_of(q);
             mbar_wait(info_full + 8 * s, parity_of(q), &sm.dead);
             Running run;
-            float bound = kNegInf;
+            float bound = INFINITY;  // TOP: the alternatives', while there is none
             if (sm.info[s].live) {
-                const Slice<T> slice = slice_at(sm.info[s].row.n_vec, slot_a);
-                auto next = [&] { if (++slot_a == plan.chunks) slot_a = 0, phase_a ^= 1; };
-                if constexpr (TOP) {
-                    const int lead = sm.info[s].row.lead, need = (a.k + kWarps - 1) / kWarps - 1;
-                    Key* list = sh.list[s];
-                    float* bounds = sh.bound[q & 1];
-                    bool some = false;  // a bound is known
-                    slice.template each<4>(
-                        [&](int slot) { mbar_wait(full + 8 * slot, phase_a, &sm.dead); },
-                        [&](auto count, const uint4* r, int v, bool) {
+                const Row<T>& row = sm.info[s].row;
+                const Slice<T> slice = slice_at(row.n_vec);
+                const int chunks = slice.chunks();
+                for (int k = 0; k < chunks; ++k) {
+                    const uint8_t* data = chunk_here();
+                    if constexpr (TOP) {
+                        const int lead = row.lead, size = TopShared::list_size(a.k);
+                        Key* list = sh.list(s, a.k);
+                        slice.template each<4>(data, k, [&](auto count, const uint4* r, int v, bool) {
                             run.add<T, ENT, decltype(count)::n>(r, c);
-                            if (some) collect<T, decltype(count)::n>(r, v, lead, bound, list, &sh.n[s]);
-                        },
-                        [&](int slot, int k) {
-                            if ((k & (k + 1)) == 0) {  // after 1, 2, 4, ... chunks
-                                const float own = warp_kth(run.m, need);
-                                if (lane == 0) *(volatile float*)&bounds[warp] = own;
-                                if (k == 0)
-                                    row_threads_sync();
-                                else
-                                    __syncwarp();
-                                float b = lane < kWarps ? *(volatile float*)&bounds[lane] : INFINITY;
+                            if (k > 0) collect<T, decltype(count)::n>(r, v, lead, bound, list, size, &sh.n[s]);
+                        });
+                        *(volatile float*)&sh.most[s][tid] = run.m;
+                        if (k == 0) {
+                            float* firsts = sh.first[q & 1];
+                            const float own = warp_kth(run.m, (a.k + kWarps - 1) / kWarps - 1);
+                            if (lane == 0) firsts[warp] = own;
+                            row_threads_sync();
+                            bound = firsts[lane % kWarps];
 #pragma unroll
-                                for (int off = 16; off; off >>= 1) b = fminf(b, __shfl_xor_sync(0xffffffffu, b, off));
-                                bound = b;
-                                some = true;
-                                if (k == 0)
-                                    slice.template chunk_of<1>(slot, 0, [&](Count<1>, const uint4* r, int v, bool) {
-                                        collect<T, 1>(r, v, lead, bound, list, &sh.n[s]);
-                                    });
-                            }
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(empty + 8 * slot);
-                            next();
-                        });
-                    row_threads_sync();
-                    if (sh.n[s] > kList) {
-                        row_threads_sync();
-                        collect_exact(sm.info[s].row, first, slice.n, a.k, sh, list, &sh.n[s]);
-                        bound = kNegInf;
+                            for (int off = 16; off; off >>= 1) bound = fminf(bound, __shfl_xor_sync(0xffffffffu, bound, off));
+                            slice.template each<1>(data, 0, [&](Count<1>, const uint4* r, int v, bool) {
+                                collect<T, 1>(r, v, lead, bound, list, size, &sh.n[s]);
+                            });
+                        } else {
+                            bound = fmaxf(bound, *(volatile float*)&sh.bound[s]);
+                        }
                     } else {
-                        bound = warp_kth(run.m, need);
-                    }
-                } else {
-                    slice.template each<4>(
-                        [&](int slot) { mbar_wait(full + 8 * slot, phase_a, &sm.dead); },
-                        [&](auto count, const uint4* r, int, bool) { run.add<T, ENT, decltype(count)::n>(r, c); },
-                        [&](int slot, int) {
-                            if (!RES) {
-                                __syncwarp();
-                                if (lane == 0) mbar_arrive(empty + 8 * slot);
-                            }
-                            next();
+                        slice.template each<4>(data, k, [&](auto count, const uint4* r, int, bool) {
+                            run.add<T, ENT, decltype(count)::n>(r, c);
                         });
+                    }
+                    chunk_done();
+                }
+                if constexpr (TOP) {
+                    row_threads_sync();
+                    if (sh.n[s] > TopShared::list_size(a.k)) {
+                        row_threads_sync();
+                        collect_exact(row, first, slice.n, a.k, sh, sh.list(s, a.k), &sh.n[s]);
+                        bound = kNegInf;
+                    }
                 }
             }
             Stats st = run.stats();
             st.join_warp<ENT>(c);
-            if (!RES && q >= 2) mbar_wait(coef_full + 8 * slot_of(q - 2), parity_of(q - 2), &sm.dead);  // (as RES does in rest)
+            const bool low = GRAD && ENT && __any_sync(0xffffffffu, run.low);
+            // (a gradient waits for its row's, see there: no CTA of the cluster is more than three rows ahead of a helper)
+            if (!GRAD && q >= 2) mbar_wait(coef_full + 8 * slot_of(q - 2), parity_of(q - 2), &sm.dead);
             if (tid == 0) mbar_expect(parts_full + 8 * s, cta_n * kWarps * 16);
             if (lane < cta_n)
-                send(map_to(smem_addr(&sm.parts[s][rank][warp]), lane), map_to(parts_full + 8 * s, lane), st.m, st.s, st.t, bound);
-            if (!RES) {
+                send(map_to(smem_addr(&sm.parts[s][rank][warp]), lane), map_to(parts_full + 8 * s, lane), st.m, st.s, st.t,
+                     TOP ? bound : low ? 1.f : 0.f);
+            if (!GRAD) {
                 __syncwarp();
                 if (lane == 0) mbar_arrive(info_empty + 8 * s);
             }
@@ -1068,51 +1203,55 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             const int s = slot_of(q);
             const RowInfo<T>& info = sm.info[s];
             const Row<T> row = info.row;
-            const Slice<T> slice = slice_at(row.n_vec, slot_b);
+            const Slice<T> slice = slice_at(row.n_vec);
             mbar_wait(coef_full + 8 * s, parity_of(q), &sm.dead);
             const Coef f = sm.coef[s];
             if (!info.live) {
                 const uint4 zero = make_uint4(0, 0, 0, 0);
                 for (int g = warp * 32; g < slice.n; g += kRowThreads) row.store(first + g + lane, zero, g + lane < slice.n);
             } else {
-                const F2 base(-f.m, -f.m), c2(c, c), less(-f.log2_s, -f.log2_s), k02(f.k0, f.k0), k12(f.k1, f.k1);
+                const F2 c2(c, c), less(-f.log2_s, -f.log2_s), k02(f.k0, f.k0), k12(f.k1, f.k1);
+                auto gradient = [&](const uint4& r, bool low) {
+                    F2 d[E / 2];
+                    float y[E];
+                    Vec<T>::minus(r, f.m, d);
+#pragma unroll
+                    for (int e = 0; e < E / 2; ++e) {
+                        d[e] = fma2(d[e], c2, less);
+                        const F2 p = exp2_of(d[e]);
+                        if (ENT && low) d[e] = d[e].at_least(-1e30f);
+                        (p * (ENT ? fma2(k12, d[e], k02) : k02)).get(y[2 * e], y[2 * e + 1]);
+                    }
+                    return Vec<T>::pack(y);
+                };
                 // a warp's vectors are all whole from plain_lo on and before plain_hi
-                const int plain_lo = row.whole_lo + lane, plain_hi = row.whole_lo + row.whole_n + lane - 31;
+                const bool plain = row.shift == 0 && !f.low;
+                const int plain_lo = plain ? row.whole_lo + lane : row.n_vec, plain_hi = row.whole_lo + row.whole_n + lane - 31;
                 T* const dst0 = row.dx - row.lead;
-                slice.template each<2>(
-                    [](int) {},
-                    [&](auto count, const uint4* r, int v, bool act) {
+                const int chunks = slice.chunks();
+                for (int k = 0; k < chunks; ++k) {
+                    slice.template each<2>(chunk_here(), k, [&](auto count, const uint4* r, int v, bool act) {
                         constexpr int N = decltype(count)::n;
-                        static_assert(N <= 2);
-                        uint4 out[N];
-#pragma unroll
-                        for (int u = 0; u < N; ++u) {
-                            float y[E];
-                            Vec<T>::unpack(r[u], y);
-#pragma unroll
-                            for (int e = 0; e < E; e += 2) {
-                                float d0, d1;
-                                fma2(F2(y[e], y[e + 1]) + base, c2, less).get(d0, d1);
-                                const F2 p(exp2_approx(d0), exp2_approx(d1));
-                                (p * (ENT ? fma2(k12, F2(fmaxf(d0, -1e30f), fmaxf(d1, -1e30f)), k02) : k02)).get(y[e], y[e + 1]);
-                            }
-                            out[u] = Vec<T>::pack(y);
-                        }
-                        if (row.shift == 0 && v >= plain_lo && v + (N - 1) * kRowThreads < plain_hi) {
+                        if (v >= plain_lo && v + (N - 1) * kRowThreads < plain_hi) {
                             T* dst = dst0 + v * E;
 #pragma unroll
-                            for (int u = 0; u < N; ++u)
-                                if (N > 1 || act) *(uint4*)(dst + u * kRowThreads * E) = out[u];
+                            for (int u = 0; u < N; ++u) {
+                                const uint4 y = gradient(r[u], false);
+                                if (N > 1 || act) __stcs((uint4*)(dst + u * kRowThreads * E), y);
+                            }
                         } else {
 #pragma unroll 1
-                            for (int u = 0; u < N; ++u) row.store(v + u * kRowThreads, u == 0 ? out[0] : out[N - 1], act);
+                            for (int u = 0; u < N; ++u) {
+                                uint4 x = r[0];
+#pragma unroll
+                                for (int w = 1; w < N; ++w)
+                                    if (u == w) x = r[w];
+                                row.store(v + u * kRowThreads, gradient(x, true), act);
+                            }
                         }
-                    },
-                    [&](int slot, int) {
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(empty + 8 * slot);
-                        if (++slot_b == plan.chunks) slot_b = 0;
                     });
+                    chunk_done();
+                }
                 // the tokens that have a term of their own again, each by the warp that stored its vector
                 if (f.terms) {
                     auto mine = [&](int id) {
@@ -1146,18 +1285,9 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
             if (lane == 0) mbar_arrive(info_empty + 8 * s);
         };
 
-        if constexpr (!RES) {
-            for (int q = 0; q < rows; ++q) statistics(q);
-        } else if (plan.ahead) {
-            for (int q = 0; q <= rows; ++q) {
-                if (q < rows) statistics(q);
-                if (q > 0) rest(q - 1);
-            }
-        } else {
-            for (int q = 0; q < rows; ++q) {
-                statistics(q);
-                rest(q);
-            }
+        for (int q = 0; q < rows; ++q) {
+            statistics(q);
+            if constexpr (GRAD) rest(q);
         }
     }
     __syncwarp();
@@ -1234,52 +1364,75 @@ cudaError_t by_type(const RowArgs& a, F f) {
     return f(__nv_bfloat16{});
 }
 
-// The cluster and ring of a call. A row's slice of at most a third of the ring bytes leaves
-// room for the next row's and a part of the one after; fewer CTAs a row exchange less.
-constexpr int kSms = 152;
-constexpr int kMaxChunkVecs = 2048;
+// The cluster and ring of a call.
+struct Shape {
+    int n, n_vec, k;  // rows, vectors of the longest row, alternatives or teacher logits
+    int fixed;        // bytes of static shared memory
+    bool grad, top, teacher;
+};
+struct Launch {
+    Plan plan;
+    int clusters, smem;  // smem: dynamic
+};
 
-template <typename T, int OP, bool RES, bool ENT, bool TOP = false>
+// Two CTAs share an SM, so that one works while the other waits. Fewer CTAs a row
+// exchange less, but a gradient's rows at work have to stay in L2 together with what
+// is written meanwhile: at most kRowsInL2 of them. Few rows are spread over more
+// CTAs, down to slices of 8 KB. Long lists of alternatives leave room for one CTA an
+// SM only. False: too large.
+bool make_launch(const Shape& h, Launch& out) {
+    constexpr int kSms = 152, kSmBytes = 233472, kMaxBytes = 232448, kReserved = 1024;
+    constexpr int64_t kRowsInL2 = 48ll << 20;
+    constexpr int kChunkVecs = 4 * kRowThreads, kAtLeast = 3 * kChunkVecs * 16;  // of a ring
+    // clusters of 1, 2, 4 and 8 CTAs that the GPU holds at once, one or two CTAs an SM
+    static const int kClusters[2][4] = {{152, 76, 36, 15}, {304, 152, 74, 36}};
+    const int half = kSmBytes / 2 - kReserved - h.fixed, whole = kMaxBytes - h.fixed;
+    Plan& plan = out.plan;
+    int size = 0;  // log2 of the CTAs a row
+    for (; size < 3; ++size) {
+        const int64_t slice = (int64_t)(h.n_vec + (1 << size) - 1) / (1 << size) * 16;
+        const bool spread = (int64_t)h.n * 2 << size <= kSms && slice > 8192;
+        const bool far = h.grad && (int64_t)std::min(h.n, kClusters[1][size]) * h.n_vec * 16 > kRowsInL2;
+        if (!spread && !far) break;
+    }
+    plan.cta_n = 1 << size;
+    plan.per_cta = (h.n_vec + plan.cta_n - 1) / plan.cta_n;
+    const int behind = h.top ? TopShared::bytes(h.k, plan.cta_n)
+                             : h.teacher ? kHelpers * kSeenWords * 4 + kSlots * h.k * TeacherList::kBytes : 0;
+    // chunks of four vectors a working thread, or a little more where that saves one
+    const int parts = (plan.per_cta + kChunkVecs * 33 / 32 - 1) / (kChunkVecs * 33 / 32);
+    const int even = ((plan.per_cta + parts - 1) / parts + 31) / 32 * 32;
+    plan.chunk = parts > 1 ? std::max(even, kChunkVecs) : even;
+    const bool two = half - behind >= kAtLeast;
+    plan.chunks = std::min(kMaxChunks, ((two ? half : whole) - behind) / (plan.chunk * 16));
+    out.clusters = std::min(h.n, kClusters[two][size]);
+    out.smem = plan.chunks * plan.chunk * 16 + behind;
+    return plan.chunks >= 2 && out.smem <= whole;
+}
+
+template <typename T, int OP, bool GRAD, bool ENT, bool TOP = false>
 cudaError_t launch_rows(const RowArgs& a, cudaStream_t s) {
     constexpr int E = Vec<T>::E;
-    constexpr int kMost = 232448 - (int)sizeof(RowShared<T>) - 1024;
-    const int behind = TOP ? (int)sizeof(TopShared) : OP == OP_DISTILL ? kHelpers * kSeenWords * 4 + kSlots * a.k * TeacherList::kBytes : 0;
-    const int room = kMost - behind;
     // (rows that all begin in a line of their own have one vector less than rows at any place)
     const bool lines = (uintptr_t)a.x % 16 == 0 && (a.n == 1 || a.x_stride % E == 0);
-    const int n_vec = (a.vocab + (lines ? 1 : 2) * (E - 1)) / E;
-    Plan plan;
-    plan.cta_n = 1;
-    while (plan.cta_n < kMaxCluster) {
-        const int64_t slice = (int64_t)(n_vec + plan.cta_n - 1) / plan.cta_n * 16;
-        if (!(RES && slice > room / 3) && !((int64_t)a.n * plan.cta_n * 2 <= kSms && slice > 8192)) break;
-        plan.cta_n *= 2;
-    }
-    plan.per_cta = (n_vec + plan.cta_n - 1) / plan.cta_n;
-    const int parts = std::max(1, (plan.per_cta + kMaxChunkVecs / 4) / kMaxChunkVecs);
-    plan.chunk = ((plan.per_cta + parts - 1) / parts + 31) / 32 * 32;
-    plan.chunks = std::min(kMaxChunks, room / (plan.chunk * 16));
-    const int own = (plan.per_cta + plan.chunk - 1) / plan.chunk;
-    plan.ahead = !RES || 2 * own <= plan.chunks;
-    if (RES && own > plan.chunks) return cudaErrorInvalidValue;
-    auto kernel = wide_kernel<T, OP, RES, ENT, TOP>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+    const Shape shape{a.n, (a.vocab + (lines ? 1 : 2) * (E - 1)) / E, a.k, (int)sizeof(RowShared<T>), GRAD, TOP, OP == OP_DISTILL};
+    Launch l;
+    if (!make_launch(shape, l)) return cudaErrorInvalidConfiguration;
+    auto kernel = wide_kernel<T, OP, GRAD, ENT, TOP>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, l.smem);
     if (e != cudaSuccess) return e;
-    static const int kClusters[4] = {152, 76, 36, 15};  // of 1, 2, 4 and 8 CTAs that the GPU holds at once
-    const int at = plan.cta_n == 1 ? 0 : plan.cta_n == 2 ? 1 : plan.cta_n == 4 ? 2 : 3;
-    const int64_t clusters = std::min<int64_t>(a.n, kClusters[at]);
     cudaLaunchAttribute attr[1] = {};
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = plan.cta_n;
+    attr[0].val.clusterDim.x = l.plan.cta_n;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(clusters * plan.cta_n));
+    cfg.gridDim = dim3((unsigned)(l.clusters * l.plan.cta_n));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = (size_t)plan.chunks * plan.chunk * 16 + behind;
+    cfg.dynamicSmemBytes = (size_t)l.smem;
     cfg.stream = s;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, a, plan);
+    return cudaLaunchKernelEx(&cfg, kernel, a, l.plan);
 }
 
 template <typename T, bool ENT>
