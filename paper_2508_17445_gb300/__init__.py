@@ -493,38 +493,49 @@ def _float_code(t) -> int:
     return c
 
 
-def _rows(t, n: int, vocab: int, code: int, device) -> int:
+def _rows(t, n: int, vocab: int, code: int, device: int) -> int:
     """Elements between the rows of [n][vocab] tensor ``t``."""
-    if t.dim() != 2 or t.shape[0] != n or t.shape[1] != vocab or _code(t) != code or t.device != device:
+    if t.shape != (n, vocab) or _code(t) != code or t.get_device() != device:
         raise ValueError("dlogits must have the logits' shape, type and device")
-    s = t.stride()
-    if s[1] != 1 and vocab > 1:
+    s0, s1 = t.stride()
+    if s1 != 1 and vocab > 1:
         raise ValueError("the elements of a row must be contiguous")
-    return s[0] if n > 1 else max(s[0], vocab)
+    return s0 if n > 1 else max(s0, vocab)
 
 
 def _logits(t, temperature: float) -> TpLogits:
     if t.dim() != 2 or not t.is_cuda:
         raise ValueError("logits must be a CUDA tensor of shape [n][vocab]")
     n, v = t.shape
-    code = _float_code(t)
-    return TpLogits(t.data_ptr(), _rows(t, n, v, code, t.device) if v else 0, n, v, code, temperature)
+    s0, s1 = t.stride()
+    if s1 != 1 and v > 1:
+        raise ValueError("the elements of a row must be contiguous")
+    return TpLogits(t.data_ptr(), s0 if n > 1 else max(s0, v), n, v, _float_code(t), temperature)
 
 
-def _row_values(t, name: str, shape, device, int32: bool = False):
+def _row_values(t, name: str, shape, device: int, code: int = TP_F32):
     """Pointer of a contiguous fp32 (int32) tensor of this shape, or None."""
     if t is None:
         return None
-    if t.shape != shape or t.device != device or not t.is_contiguous() or _code(t) != (_INT32 if int32 else TP_F32):
-        raise ValueError(f"{name} must be a contiguous {'int32' if int32 else 'fp32'} tensor {list(shape)} on the logits' device")
+    if t.shape != shape or t.get_device() != device or _code(t) != code or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {'int32' if code == _INT32 else 'fp32'} tensor {list(shape)} on the "
+                         "logits' device")
     return t.data_ptr()
 
 
-def _stream_of(t, stream) -> int:
+_raw_stream = None  # device index -> handle of torch's current stream
+
+
+def _stream_of(device: int, stream) -> int:
     if stream is not None:
         return getattr(stream, "cuda_stream", stream)
-    import torch
-    return torch.cuda.current_stream(t.device).cuda_stream
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        # (the handle alone; making a Stream object of it takes 2 us a call)
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda d: torch.cuda.current_stream(d).cuda_stream)
+    return _raw_stream(device)
 
 
 def tp_token_logprobs(logits, tokens=None, logp=None, entropy=None, lse=None, top_ids=None, top_logp=None,
@@ -533,17 +544,17 @@ def tp_token_logprobs(logits, tokens=None, logp=None, entropy=None, lse=None, to
     fp32 [n] or None; top_ids int32 [n][k] and top_logp fp32 [n][k] or None. Runs on ``stream`` (a torch stream or a
     raw handle), by default torch's current stream."""
     view = _logits(logits, temperature)
-    n, dev = view.n, logits.device
+    n, dev = view.n, logits.get_device()
     k = 0
     if top_ids is not None or top_logp is not None:
         if top_ids is None or top_logp is None or top_ids.dim() != 2:
             raise ValueError("top_ids and top_logp come together, [n][k]")
         k = int(top_ids.shape[1])
     st = load_library().tp_token_logprobs(
-        ctypes.byref(view), _row_values(tokens, "tokens", (n,), dev, True), _row_values(logp, "logp", (n,), dev),
+        ctypes.byref(view), _row_values(tokens, "tokens", (n,), dev, _INT32), _row_values(logp, "logp", (n,), dev),
         _row_values(entropy, "entropy", (n,), dev), _row_values(lse, "lse", (n,), dev), k,
-        _row_values(top_ids, "top_ids", (n, k), dev, True), _row_values(top_logp, "top_logp", (n, k), dev),
-        _stream_of(logits, stream))
+        _row_values(top_ids, "top_ids", (n, k), dev, _INT32), _row_values(top_logp, "top_logp", (n, k), dev),
+        _stream_of(dev, stream))
     if st:
         _check(None, st)
 
@@ -553,12 +564,12 @@ def tp_token_logprobs_backward(logits, tokens, lse, dlogits, dlogp=None, dentrop
     """dlogits: the logits' shape and type (it may be the logits); lse, entropy: tp_token_logprobs' results; dlogp,
     dentropy: fp32 [n], one may be None."""
     view = _logits(logits, temperature)
-    n, dev = view.n, logits.device
+    n, dev = view.n, logits.get_device()
     st = load_library().tp_token_logprobs_backward(
-        ctypes.byref(view), _row_values(tokens, "tokens", (n,), dev, True), _row_values(lse, "lse", (n,), dev),
+        ctypes.byref(view), _row_values(tokens, "tokens", (n,), dev, _INT32), _row_values(lse, "lse", (n,), dev),
         _row_values(entropy, "entropy", (n,), dev), _row_values(dlogp, "dlogp", (n,), dev),
         _row_values(dentropy, "dentropy", (n,), dev), _ptr(dlogits),
-        _rows(dlogits, n, view.vocab, view.dtype, dev), _stream_of(logits, stream))
+        _rows(dlogits, n, view.vocab, view.dtype, dev), _stream_of(dev, stream))
     if st:
         _check(None, st)
 
@@ -569,13 +580,13 @@ def tp_policy_loss(logits, tokens, advantage, loss, dlogits=None, old_logp=None,
     """tokens int32 [n]; advantage, old_logp, weight, loss, logp, entropy fp32 [n] (all but advantage and loss may be
     None); dlogits: the logits' shape and type (it may be the logits) or None."""
     view = _logits(logits, temperature)
-    n, dev = view.n, logits.device
+    n, dev = view.n, logits.get_device()
     st = load_library().tp_policy_loss(
-        ctypes.byref(view), _row_values(tokens, "tokens", (n,), dev, True),
+        ctypes.byref(view), _row_values(tokens, "tokens", (n,), dev, _INT32),
         _row_values(advantage, "advantage", (n,), dev), _row_values(old_logp, "old_logp", (n,), dev),
         _row_values(weight, "weight", (n,), dev), clip_low, clip_high, entropy_coef, _row_values(loss, "loss", (n,), dev),
         _row_values(logp, "logp", (n,), dev), _row_values(entropy, "entropy", (n,), dev), _ptr(dlogits),
-        0 if dlogits is None else _rows(dlogits, n, view.vocab, view.dtype, dev), _stream_of(logits, stream))
+        0 if dlogits is None else _rows(dlogits, n, view.vocab, view.dtype, dev), _stream_of(dev, stream))
     if st:
         _check(None, st)
 
@@ -585,16 +596,16 @@ def tp_distill_loss(logits, teacher_ids, teacher_logits, loss, dlogits=None, wei
     """teacher_ids int32 [n][k], teacher_logits bf16, fp16 or fp32 [n][k]; loss, weight fp32 [n] (weight may be None);
     dlogits: the logits' shape and type (it may be the logits) or None."""
     view = _logits(logits, temperature)
-    n, dev = view.n, logits.device
-    if teacher_ids.dim() != 2 or teacher_logits.shape != teacher_ids.shape or teacher_logits.device != dev or \
+    n, dev = view.n, logits.get_device()
+    if teacher_ids.dim() != 2 or teacher_logits.shape != teacher_ids.shape or teacher_logits.get_device() != dev or \
             not teacher_logits.is_contiguous():
         raise ValueError("teacher_ids and teacher_logits must be contiguous [n][k] tensors on the logits' device")
     k = int(teacher_ids.shape[1])
     st = load_library().tp_distill_loss(
-        ctypes.byref(view), _row_values(teacher_ids, "teacher_ids", (n, k), dev, True), teacher_logits.data_ptr(),
+        ctypes.byref(view), _row_values(teacher_ids, "teacher_ids", (n, k), dev, _INT32), teacher_logits.data_ptr(),
         _float_code(teacher_logits), k, _row_values(weight, "weight", (n,), dev), _row_values(loss, "loss", (n,), dev),
         _ptr(dlogits), 0 if dlogits is None else _rows(dlogits, n, view.vocab, view.dtype, dev),
-        _stream_of(logits, stream))
+        _stream_of(dev, stream))
     if st:
         _check(None, st)
 

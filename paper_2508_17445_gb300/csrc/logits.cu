@@ -27,6 +27,7 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "logits.h"
 
@@ -173,7 +174,9 @@ __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_
                  "l"(src), "r"(bytes), "r"(bar), "l"(policy)
                  : "memory");
 }
-__device__ __forceinline__ void row_threads_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kRowThreads) : "memory"); }
+template <int THREADS>
+__device__ __forceinline__ void threads_sync() { asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory"); }
+__device__ __forceinline__ void row_threads_sync() { threads_sync<kRowThreads>(); }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
@@ -534,6 +537,60 @@ struct RowShared {
     int dead;
 };
 
+// The coefficients from a row's statistics (low: some thread's), and what the row's results take: ln p of the token
+// and the policy term.
+template <int OP, bool ENT, typename T>
+__device__ __forceinline__ Coef coefficients(const RowArgs& a, const RowInfo<T>& info, const RowResult& res, bool low, float& logp,
+                                             float& term) {
+    Coef f{};
+    f.m = res.m;
+    f.log2_s = res.log2_s;
+    f.low = low;
+    logp = NAN;
+    if (OP != OP_DISTILL && info.tok < a.vocab) logp = res.logp(info.x_tok);
+    if constexpr (OP == OP_POLICY) {
+        float g;
+        term = policy_term(logp, info.adv, a.old_logp ? &info.old : nullptr, 0, a.clip_low, a.clip_high, g);
+        const float wt = info.w * res.inv_t;
+        f.k0 = wt * (ENT ? a.entropy_coef * res.entropy - g : -g);
+        f.k1 = ENT ? wt * a.entropy_coef * kLn2 : 0.f;
+        f.k2 = wt * g;
+        f.terms = info.tok < a.vocab && !res.empty;
+    }
+    if constexpr (OP == OP_DISTILL) {
+        f.k0 = info.bad ? NAN : info.w * res.inv_t;
+        f.terms = !info.bad && !isnan(res.lse) && !res.empty;
+    }
+    return f;
+}
+
+// A row's results; one thread. res of a row that is not live is not looked at.
+template <int OP, bool ENT>
+__device__ __forceinline__ void write_results(const RowArgs& a, int64_t i, bool live, float w, const RowResult& res, float logp, float term) {
+    if (OP == OP_POLICY) a.loss[i] = !live ? 0.f : w * (ENT ? term - a.entropy_coef * res.entropy : term);
+    if (OP != OP_DISTILL && a.logp) a.logp[i] = live ? logp : 0.f;
+    if (OP != OP_DISTILL && ENT && a.entropy) a.entropy[i] = live ? res.entropy : 0.f;
+    if (OP == OP_LOGPROBS && a.lse) a.lse[i] = live ? res.lse : 0.f;
+}
+
+// The gradient of a vector's logits; low: see Coef.
+template <typename T, bool ENT>
+__device__ __forceinline__ uint4 gradient(const uint4& r, const Coef& f, float c, bool low) {
+    constexpr int E = Vec<T>::E;
+    const F2 c2(c, c), less(-f.log2_s, -f.log2_s), k0(f.k0, f.k0), k1(f.k1, f.k1);
+    F2 d[E / 2];
+    float y[E];
+    Vec<T>::minus(r, f.m, d);
+#pragma unroll
+    for (int e = 0; e < E / 2; ++e) {
+        d[e] = fma2(d[e], c2, less);
+        const F2 p = exp2_of(d[e]);
+        if (ENT && low) d[e] = d[e].at_least(-1e30f);
+        (p * (ENT ? fma2(k1, d[e], k0) : k0)).get(y[2 * e], y[2 * e + 1]);
+    }
+    return Vec<T>::pack(y);
+}
+
 // The teacher's list of one row, k long each; the slots' lie behind the ring.
 struct TeacherList {
     int32_t* id;   // -1: no share
@@ -548,6 +605,41 @@ struct TeacherList {
 };
 constexpr int kSeenWords = 256;  // a bit for the tokens of equal residue, by which repeated ones are told
 
+// The tokens that have a term of their own again, each by the warp (mine(id)) that stored its vector.
+template <typename T, int OP, bool ENT, typename M>
+__device__ __forceinline__ void own_terms(const Row<T>& row, const RowInfo<T>& info, const Coef& f, float c, const TeacherList& list, M mine) {
+    const int lane = threadIdx.x & 31;
+    if (!f.terms) return;
+    if constexpr (OP == OP_POLICY) {
+        if (lane == 0 && mine(info.tok)) {
+            const float d = fmaf(c, info.x_tok - f.m, -f.log2_s), p = exp2_approx(d);
+            row.dx[info.tok] = from_f32<T>(fmaf(p, ENT ? fmaf(f.k1, fmaxf(d, -1e30f), f.k0) : f.k0, f.k2));
+        }
+    }
+    if constexpr (OP == OP_DISTILL) {
+        for (int k = lane; k < info.n_own; k += 32) {
+            const int at = list.own[k], id = list.id[at];
+            if (!mine(id)) continue;
+            float q = list.q[at];
+            if (info.repeats) {
+                q = 0.f;
+                for (int p = 0; p < info.n_own; ++p)
+                    if (list.id[list.own[p]] == id) q += list.q[list.own[p]];
+            }
+            const float d = fmaf(c, list.x[at] - f.m, -f.log2_s);
+            row.dx[id] = from_f32<T>((exp2_approx(d) - q) * f.k0);
+        }
+    }
+}
+
+// The distillation loss of a row, without the weight; one warp.
+__device__ __forceinline__ float teacher_loss(const TeacherList& list, int k, const RowResult& res) {
+    float part = 0.f;
+    for (int p = threadIdx.x & 31; p < k; p += 32)
+        if (list.id[p] >= 0) part += list.q[p] * (logf(list.q[p]) - res.logp(list.x[p]));
+    return warp_sum(part);
+}
+
 // Alternatives. A key holds a logit, in an order of unsigned integers, above the
 // complement of its id: the k largest keys are the k largest logits, of equal ones
 // the lower ids. Where k threads have met a logit of at least b, nothing below b is
@@ -559,12 +651,13 @@ constexpr int kSeenWords = 256;  // a bit for the tokens of equal residue, by wh
 // all with all, and one CTA's helper merges the cluster's. A list that overflows
 // (many equal logits, rows in rising order) is made again by finding the k-th
 // largest key by its digits.
+template <int THREADS, int SLOTS>
 struct TopShared {
-    uint64_t best_full[kSlots];
-    float most[kSlots][kRowThreads];  // the threads' largest logits so far
-    float bound[kSlots];              // what the helper has made of them
-    float first[2][kWarps];
-    int n[kSlots];
+    uint64_t best_full[SLOTS];
+    float most[SLOTS][THREADS];  // the threads' largest logits so far
+    float bound[SLOTS];          // what the helper has made of them
+    float first[2][THREADS / 32];
+    int n[SLOTS];
     int digit, rest;
     int hist[256];
     // behind it: the slots' lists of list_size(k) keys, then the first CTA's best keys of each slot and CTA: k, descending,
@@ -572,13 +665,14 @@ struct TopShared {
 
     static __host__ __device__ __forceinline__ int list_size(int k) { return 1024 + 8 * k; }
     static __host__ __forceinline__ int bytes(int k, int cta_n) {
-        return (int)sizeof(TopShared) + kSlots * 8 * (list_size(k) + (cta_n > 1 ? cta_n * k : 0));
+        return (int)sizeof(TopShared) + SLOTS * 8 * (list_size(k) + (cta_n > 1 ? cta_n * k : 0));
     }
     __device__ __forceinline__ Key* list(int s, int k) { return (Key*)(this + 1) + s * list_size(k); }
     __device__ __forceinline__ Key* best(int s, int rank, int k, int cta_n) {
-        return (Key*)(this + 1) + kSlots * list_size(k) + (s * cta_n + rank) * k;
+        return (Key*)(this + 1) + SLOTS * list_size(k) + (s * cta_n + rank) * k;
     }
 };
+typedef TopShared<kRowThreads, kSlots> WideTop;
 
 struct Plan {
     int cta_n;          // CTAs a cluster
@@ -671,11 +765,11 @@ __device__ __forceinline__ void collect(const uint4* r, int v, int lead, float b
 // The list of the slice's k largest keys, from memory; all working warps. The
 // k-th largest key is found by its digits of 8 bits, the highest first; the id's
 // highest digit is the same in all.
-template <typename T>
-__device__ __noinline__ void collect_exact(const Row<T>& row, int first, int n, int k, TopShared& sh, Key* list, int* count) {
+template <int THREADS, typename T, typename S>
+__device__ __noinline__ void collect_exact(const Row<T>& row, int first, int n, int k, S& sh, Key* list, int* count) {
     constexpr int E = Vec<T>::E;
     auto each_key = [&](auto f) {
-        for (int v = first + threadIdx.x; v < first + n; v += kRowThreads) {
+        for (int v = first + threadIdx.x; v < first + n; v += THREADS) {
             float x[E];
             Vec<T>::unpack(row.load(v), x);
 #pragma unroll
@@ -691,12 +785,12 @@ __device__ __noinline__ void collect_exact(const Row<T>& row, int first, int n, 
             mask |= (Key)0xff << 24;
             continue;
         }
-        for (int b = threadIdx.x; b < 256; b += kRowThreads) sh.hist[b] = 0;
-        row_threads_sync();
+        for (int b = threadIdx.x; b < 256; b += THREADS) sh.hist[b] = 0;
+        threads_sync<THREADS>();
         each_key([&](Key key) {
             if ((key & mask) == found) atomicAdd(&sh.hist[(int)(key >> shift) & 255], 1);
         });
-        row_threads_sync();
+        threads_sync<THREADS>();
         if (threadIdx.x < 32) {  // lane l: digits 255 - 8 l downwards
             int sum = 0;
             for (int b = 0; b < 8; ++b) sum += sh.hist[255 - 8 * threadIdx.x - b];
@@ -718,29 +812,30 @@ __device__ __noinline__ void collect_exact(const Row<T>& row, int first, int n, 
                 sh.rest = rest - before;
             }
         }
-        row_threads_sync();
+        threads_sync<THREADS>();
         found |= (Key)sh.digit << shift;
         mask |= (Key)0xff << shift;
         rest = sh.rest;
     }
     if (threadIdx.x == 0) *count = 0;
-    row_threads_sync();
+    threads_sync<THREADS>();
     each_key([&](Key key) {
         if (key >= found) {
             const int at = atomicAdd(count, 1);
             list[at] = key;  // (k of them)
         }
     });
-    row_threads_sync();
+    threads_sync<THREADS>();
 }
 
 // One helper warp: a value, at least b, that k of the threads' maxima are not below (b or -inf where there are fewer).
 // Halving between the largest and b, in the order of keys, until at most k / 8 too many are left.
+template <int THREADS>
 __device__ __forceinline__ float kth_of_maxima(const float* most, int k, float b) {
     const int lane = threadIdx.x & 31;
-    uint32_t v[kRowThreads / 32], lo = (uint32_t)(make_key(b, 0) >> 32), hi = lo;
+    uint32_t v[THREADS / 32], lo = (uint32_t)(make_key(b, 0) >> 32), hi = lo;
 #pragma unroll
-    for (int j = 0; j < kRowThreads / 32; ++j) {
+    for (int j = 0; j < THREADS / 32; ++j) {
         v[j] = (uint32_t)(make_key(((volatile const float*)most)[lane + 32 * j], 0) >> 32);
         hi = max(hi, v[j]);
     }
@@ -749,7 +844,7 @@ __device__ __forceinline__ float kth_of_maxima(const float* most, int k, float b
         const uint32_t mid = lo + (hi - lo) / 2;
         uint32_t n = 0;
 #pragma unroll
-        for (int j = 0; j < kRowThreads / 32; ++j) n += v[j] >= mid;
+        for (int j = 0; j < THREADS / 32; ++j) n += v[j] >= mid;
         n = __reduce_add_sync(0xffffffffu, n);
         if ((int)n < k) {
             hi = mid;
@@ -762,12 +857,13 @@ __device__ __forceinline__ float kth_of_maxima(const float* most, int k, float b
 }
 
 // One helper warp: the row's alternatives from the CTAs' lists. bound: nothing below it is one of them.
-__device__ __forceinline__ void alternatives(const RowArgs& a, int64_t i, TopShared& sh, int s, uint32_t parity, uint32_t rank, int cta_n,
+template <int THREADS, typename S>
+__device__ __forceinline__ void alternatives(const RowArgs& a, int64_t i, S& sh, int s, uint32_t parity, uint32_t rank, int cta_n,
                                              float bound, const RowResult& r, volatile int* dead) {
     const int lane = threadIdx.x & 31, k = a.k;
     Key* list = sh.list(s, k);
-    const int met = min(sh.n[s], TopShared::list_size(k));
-    if (met > 2 * k + 32) bound = fmaxf(bound, kth_of_maxima(sh.most[s], k, bound));
+    const int met = min(sh.n[s], S::list_size(k));
+    if (met > 2 * k + 32) bound = fmaxf(bound, kth_of_maxima<THREADS>(sh.most[s], k, bound));
     const Key least = bound > kNegInf ? make_key(bound, 0x7fffffff) : 0;  // of its equals the last
     int m = 0;
     for (int p0 = 0; p0 < met; p0 += 32) {  // left out in place: never written ahead of what is read
@@ -922,7 +1018,7 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
     auto parity_of = [](int q) { return (uint32_t)(q / kSlots) & 1; };
     // behind the ring
     uint8_t* const behind = ring + plan.chunks * slot_bytes;
-    TopShared& sh = *(TopShared*)behind;
+    WideTop& sh = *(WideTop*)behind;
     uint32_t* const seen = (uint32_t*)behind;
     auto list_at = [&](int slot) {
         return TeacherList(behind + kHelpers * kSeenWords * 4 + slot * a.k * TeacherList::kBytes, a.k);
@@ -1006,7 +1102,7 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
             if constexpr (TOP) {
                 float b = kNegInf;
                 while (plan.per_cta > plan.chunk && !mbar_try(parts_full + 8 * s, parity_of(q)) && !*(volatile int*)&sm.dead) {
-                    b = kth_of_maxima(sh.most[s], a.k, b);
+                    b = kth_of_maxima<kRowThreads>(sh.most[s], a.k, b);
                     if (lane == 0) *(volatile float*)&sh.bound[s] = b;
                     __syncwarp();
                 }
@@ -1046,44 +1142,17 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
             }
             const RowResult res(all, c, inv_t);
             const bool live = info.live;
-            Coef f{};
-            float logp = NAN, term = 0.f;
-            if (OP != OP_DISTILL && info.tok < row.vocab) logp = res.logp(info.x_tok);
-            if constexpr (OP == OP_POLICY) {
-                float g;
-                term = policy_term(logp, info.adv, a.old_logp ? &info.old : nullptr, 0, a.clip_low, a.clip_high, g);
-                const float wt = info.w * inv_t;
-                f.k0 = wt * (ENT ? a.entropy_coef * res.entropy - g : -g);
-                f.k1 = ENT ? wt * a.entropy_coef * kLn2 : 0.f;
-                f.k2 = wt * g;
-                f.low = __any_sync(0xffffffffu, low);
-                f.terms = info.tok < row.vocab && !res.empty;
-            }
-            if constexpr (OP == OP_DISTILL) {
-                f.k0 = info.bad ? NAN : info.w * inv_t;
-                f.terms = !info.bad && !isnan(res.lse) && !res.empty;
-            }
+            float logp, term = 0.f;
+            const Coef f = coefficients<OP, ENT>(a, info, res, __any_sync(0xffffffffu, low), logp, term);
             if (lane == 0) {
-                f.m = res.m;
-                f.log2_s = res.log2_s;
                 sm.coef[s] = f;
                 mbar_arrive(coef_full + 8 * s);
+                if (rank == 0) write_results<OP, ENT>(a, i, live, info.w, res, logp, term);
             }
-            if (rank == 0 && lane == 0 && OP != OP_DISTILL) {
-                if (OP == OP_POLICY) a.loss[i] = !live ? 0.f : info.w * (ENT ? term - a.entropy_coef * res.entropy : term);
-                if (a.logp) a.logp[i] = live ? logp : 0.f;
-                if (ENT && a.entropy) a.entropy[i] = live ? res.entropy : 0.f;
-                if (OP == OP_LOGPROBS && a.lse) a.lse[i] = live ? res.lse : 0.f;
-            }
-            if constexpr (TOP) alternatives(a, i, sh, s, parity_of(q), rank, cta_n, bound, res, &sm.dead);
+            if constexpr (TOP) alternatives<kRowThreads>(a, i, sh, s, parity_of(q), rank, cta_n, bound, res, &sm.dead);
             if (OP == OP_DISTILL && rank == 0) {
-                const TeacherList list = list_at(s);
-                float part = 0.f;
-                if (live && !info.bad)
-                    for (int k = lane; k < a.k; k += 32)
-                        if (list.id[k] >= 0) part += list.q[k] * (logf(list.q[k]) - res.logp(list.x[k]));
-                part = warp_sum(part);
-                if (lane == 0) a.loss[i] = !live ? 0.f : info.bad || isnan(res.lse) ? NAN : info.w * part;
+                const float loss = live && !info.bad ? teacher_loss(list_at(s), a.k, res) : 0.f;
+                if (lane == 0) a.loss[i] = !live ? 0.f : info.bad || isnan(res.lse) ? NAN : info.w * loss;
             }
             __syncwarp();
         }
@@ -1147,7 +1216,7 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
                 for (int k = 0; k < chunks; ++k) {
                     const uint8_t* data = chunk_here();
                     if constexpr (TOP) {
-                        const int lead = row.lead, size = TopShared::list_size(a.k);
+                        const int lead = row.lead, size = WideTop::list_size(a.k);
                         Key* list = sh.list(s, a.k);
                         slice.template each<4>(data, k, [&](auto count, const uint4* r, int v, bool) {
                             run.add<T, ENT, decltype(count)::n>(r, c);
@@ -1177,9 +1246,9 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
                 }
                 if constexpr (TOP) {
                     row_threads_sync();
-                    if (sh.n[s] > TopShared::list_size(a.k)) {
+                    if (sh.n[s] > WideTop::list_size(a.k)) {
                         row_threads_sync();
-                        collect_exact(row, first, slice.n, a.k, sh, sh.list(s, a.k), &sh.n[s]);
+                        collect_exact<kRowThreads>(row, first, slice.n, a.k, sh, sh.list(s, a.k), &sh.n[s]);
                         bound = kNegInf;
                     }
                 }
@@ -1210,20 +1279,6 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
                 const uint4 zero = make_uint4(0, 0, 0, 0);
                 for (int g = warp * 32; g < slice.n; g += kRowThreads) row.store(first + g + lane, zero, g + lane < slice.n);
             } else {
-                const F2 c2(c, c), less(-f.log2_s, -f.log2_s), k02(f.k0, f.k0), k12(f.k1, f.k1);
-                auto gradient = [&](const uint4& r, bool low) {
-                    F2 d[E / 2];
-                    float y[E];
-                    Vec<T>::minus(r, f.m, d);
-#pragma unroll
-                    for (int e = 0; e < E / 2; ++e) {
-                        d[e] = fma2(d[e], c2, less);
-                        const F2 p = exp2_of(d[e]);
-                        if (ENT && low) d[e] = d[e].at_least(-1e30f);
-                        (p * (ENT ? fma2(k12, d[e], k02) : k02)).get(y[2 * e], y[2 * e + 1]);
-                    }
-                    return Vec<T>::pack(y);
-                };
                 // a warp's vectors are all whole from plain_lo on and before plain_hi
                 const bool plain = row.shift == 0 && !f.low;
                 const int plain_lo = plain ? row.whole_lo + lane : row.n_vec, plain_hi = row.whole_lo + row.whole_n + lane - 31;
@@ -1236,7 +1291,7 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
                             T* dst = dst0 + v * E;
 #pragma unroll
                             for (int u = 0; u < N; ++u) {
-                                const uint4 y = gradient(r[u], false);
+                                const uint4 y = gradient<T, ENT>(r[u], f, c, false);
                                 if (N > 1 || act) __stcs((uint4*)(dst + u * kRowThreads * E), y);
                             }
                         } else {
@@ -1246,40 +1301,16 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
 #pragma unroll
                                 for (int w = 1; w < N; ++w)
                                     if (u == w) x = r[w];
-                                row.store(v + u * kRowThreads, gradient(x, true), act);
+                                row.store(v + u * kRowThreads, gradient<T, ENT>(x, f, c, true), act);
                             }
                         }
                     });
                     chunk_done();
                 }
-                // the tokens that have a term of their own again, each by the warp that stored its vector
-                if (f.terms) {
-                    auto mine = [&](int id) {
-                        const int v = (id + row.lead) / E - first;
-                        return v >= 0 && v < slice.n && v % plan.chunk / 32 % kWarps == warp;
-                    };
-                    if constexpr (OP == OP_POLICY) {
-                        if (lane == 0 && mine(info.tok)) {
-                            const float d = fmaf(c, info.x_tok - f.m, -f.log2_s), p = exp2_approx(d);
-                            row.dx[info.tok] = from_f32<T>(fmaf(p, ENT ? fmaf(f.k1, fmaxf(d, -1e30f), f.k0) : f.k0, f.k2));
-                        }
-                    }
-                    if constexpr (OP == OP_DISTILL) {
-                        const TeacherList list = list_at(s);
-                        for (int k = lane; k < info.n_own; k += 32) {
-                            const int at = list.own[k], id = list.id[at];
-                            if (!mine(id)) continue;
-                            float q = list.q[at];
-                            if (info.repeats) {
-                                q = 0.f;
-                                for (int p = 0; p < info.n_own; ++p)
-                                    if (list.id[list.own[p]] == id) q += list.q[list.own[p]];
-                            }
-                            const float d = fmaf(c, list.x[at] - f.m, -f.log2_s);
-                            row.dx[id] = from_f32<T>((exp2_approx(d) - q) * f.k0);
-                        }
-                    }
-                }
+                own_terms<T, OP, ENT>(row, info, f, c, list_at(s), [&](int id) {
+                    const int v = (id + row.lead) / E - first;
+                    return v >= 0 && v < slice.n && v % plan.chunk / 32 % kWarps == warp;
+                });
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(info_empty + 8 * s);
@@ -1293,6 +1324,137 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
     __syncwarp();
     cluster_arrive();  // (nothing is sent to a CTA that has ended)
     cluster_wait();
+}
+
+// ------------------------------------------------------------- short rows --
+// A row of at most kNarrowBytes is taken by TEAM warps on their own: the plain
+// loads of many rows a SM hide one another's latency, and a row's second reading
+// comes from L1 or L2. What a row costs in wide_kernel beside its elements (about
+// 1 us of a CTA: helpers, barriers, exchange) would be most of a short row's time.
+constexpr int kNarrowWarps = 4;
+constexpr int kNarrowBytes = 16384;
+typedef TopShared<kNarrowWarps * 32, 1> NarrowTop;
+
+template <typename T, int OP, bool GRAD, bool ENT, bool TOP, int TEAM>
+__global__ void __launch_bounds__(kNarrowWarps * 32) narrow_kernel(const __grid_constant__ RowArgs a) {
+    extern __shared__ __align__(16) uint8_t space[];
+    constexpr int kRows = kNarrowWarps / TEAM, kTeam = TEAM * 32;
+    static_assert(!TOP || TEAM == kNarrowWarps);
+    __shared__ RowInfo<T> infos[kRows];
+    __shared__ float4 parts[kNarrowWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, team = warp / TEAM, t = threadIdx.x - team * kTeam;
+    const int64_t i = (int64_t)blockIdx.x * kRows + team;
+    if (i >= a.n) return;  // (a whole warp, and with one row a CTA none)
+    auto sync = [] {
+        if constexpr (TEAM == 1)
+            __syncwarp();
+        else
+            __syncthreads();
+    };
+    const float c = kLog2e / a.temperature, inv_t = 1.f / a.temperature;
+    const Row<T> row(a, i);
+    RowInfo<T>& info = infos[team];
+    const int list_bytes = kSeenWords * 4 + a.k * TeacherList::kBytes;
+    uint32_t* seen = (uint32_t*)(space + team * list_bytes);
+    const TeacherList list(space + team * list_bytes + kSeenWords * 4, a.k);
+    NarrowTop& sh = *(NarrowTop*)space;
+    if constexpr (OP == OP_DISTILL) {
+        if (t < 32) {
+            for (int k = lane; k < kSeenWords; k += 32) seen[k] = 0;
+            __syncwarp();
+            teacher_ahead(a, i, row, 0, row.n_vec, 0, info, list, seen);
+        }
+    } else if (t == 0) {
+        const int32_t tok = a.tokens ? a.tokens[i] : 0;
+        info.tok = tok;
+        info.live = tok >= 0;
+        info.x_tok = a.tokens && tok >= 0 && tok < a.vocab ? to_f32(row.x[tok]) : NAN;  // (before a gradient in place)
+        info.w = a.weight ? a.weight[i] : 1.f;
+        if (OP == OP_POLICY) {
+            info.adv = a.advantage[i];
+            info.old = a.old_logp ? a.old_logp[i] : 0.f;
+        }
+    }
+    if constexpr (TOP)
+        if (t == 0) sh.n[0] = 0;
+    sync();
+    // f(Count<M>, M vectors kTeam apart, the first's number) over the row; the warp's lanes together, a vector past the end is -inf
+    auto each = [&](auto f) {
+        int g = t - lane;
+        for (; g + 3 * kTeam < row.n_vec; g += 4 * kTeam) {
+            uint4 r[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                r[u] = make_uint4(Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone);
+                if (g + u * kTeam + lane < row.n_vec) r[u] = row.load(g + u * kTeam + lane);
+            }
+            f(Count<4>{}, r, g + lane);
+        }
+        for (; g < row.n_vec; g += kTeam) {
+            uint4 r = make_uint4(Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone);
+            if (g + lane < row.n_vec) r = row.load(g + lane);
+            f(Count<1>{}, &r, g + lane);
+        }
+    };
+    Running run;
+    const bool live = info.live;
+    if (live) each([&](auto count, const uint4* r, int) { run.add<T, ENT, decltype(count)::n>(r, c); });
+    Stats all = run.stats();
+    all.join_warp<ENT>(c);
+    bool low = GRAD && ENT && __any_sync(0xffffffffu, run.low);
+    if constexpr (TEAM > 1) {
+        if (lane == 0) parts[warp] = make_float4(all.m, all.s, all.t, low ? 1.f : 0.f);
+        if constexpr (TOP) sh.most[0][t] = run.m;
+        sync();
+        const float4 p = parts[lane % TEAM];
+        all.m = p.x, all.s = lane < TEAM ? p.y : 0.f, all.t = lane < TEAM ? p.z : 0.f;
+        all.join_warp<ENT>(c);
+        low = __any_sync(0xffffffffu, p.w != 0.f);
+    }
+    const RowResult res(all, c, inv_t);
+    float logp, term = 0.f;
+    const Coef f = coefficients<OP, ENT>(a, info, res, low, logp, term);
+    if (t == 0) write_results<OP, ENT>(a, i, live, info.w, res, logp, term);
+    if (OP == OP_DISTILL && t < 32) {
+        const float loss = live && !info.bad ? teacher_loss(list, a.k, res) : 0.f;
+        if (lane == 0) a.loss[i] = !live ? 0.f : info.bad || isnan(res.lse) ? NAN : info.w * loss;
+    }
+    if constexpr (GRAD) {
+        if (live)
+            each([&](auto count, const uint4* r, int v) {
+#pragma unroll
+                for (int u = 0; u < decltype(count)::n; ++u)
+                    row.store(v + u * kTeam, gradient<T, ENT>(r[u], f, c, low), v + u * kTeam < row.n_vec);
+            });
+        else
+            for (int g = t - lane; g < row.n_vec; g += kTeam)
+                row.store(g + lane, make_uint4(0, 0, 0, 0), g + lane < row.n_vec);
+        __syncwarp();
+        if (live)
+            own_terms<T, OP, ENT>(row, info, f, c, list,
+                                  [&](int id) { return (id + row.lead) / Vec<T>::E / 32 % TEAM == warp % TEAM; });
+    }
+    if constexpr (TOP) {
+        Key* keys = sh.list(0, a.k);
+        float bound = kNegInf;
+        if (live) {
+            bound = kth_of_maxima<kTeam>(sh.most[0], a.k, kNegInf);
+            // (a longer list takes longer to rank than to make exactly)
+            const int size = min(4 * a.k + 64, NarrowTop::list_size(a.k));
+            each([&](auto count, const uint4* r, int v) {
+#pragma unroll
+                for (int u = 0; u < decltype(count)::n; ++u)
+                    collect<T, 1>(r + u, v + u * kTeam, row.lead, bound, keys, size, &sh.n[0]);
+            });
+            sync();
+            if (sh.n[0] > size) {
+                sync();
+                collect_exact<kTeam>(row, 0, row.n_vec, a.k, sh, keys, &sh.n[0]);
+                bound = kNegInf;
+            }
+        }
+        if (warp == 0) alternatives<kTeam>(a, i, sh, 0, 0, 0, 1, bound, res, nullptr);
+    }
 }
 
 // ---------------------------------------------------------------- backward --
@@ -1364,6 +1526,8 @@ cudaError_t by_type(const RowArgs& a, F f) {
     return f(__nv_bfloat16{});
 }
 
+constexpr int kMaxBytes = 232448;  // of shared memory a CTA
+
 // The cluster and ring of a call.
 struct Shape {
     int n, n_vec, k;  // rows, vectors of the longest row, alternatives or teacher logits
@@ -1381,7 +1545,7 @@ struct Launch {
 // CTAs, down to slices of 8 KB. Long lists of alternatives leave room for one CTA an
 // SM only. False: too large.
 bool make_launch(const Shape& h, Launch& out) {
-    constexpr int kSms = 152, kSmBytes = 233472, kMaxBytes = 232448, kReserved = 1024;
+    constexpr int kSms = 152, kSmBytes = 233472, kReserved = 1024;
     constexpr int64_t kRowsInL2 = 48ll << 20;
     constexpr int kChunkVecs = 4 * kRowThreads, kAtLeast = 3 * kChunkVecs * 16;  // of a ring
     // clusters of 1, 2, 4 and 8 CTAs that the GPU holds at once, one or two CTAs an SM
@@ -1397,7 +1561,7 @@ bool make_launch(const Shape& h, Launch& out) {
     }
     plan.cta_n = 1 << size;
     plan.per_cta = (h.n_vec + plan.cta_n - 1) / plan.cta_n;
-    const int behind = h.top ? TopShared::bytes(h.k, plan.cta_n)
+    const int behind = h.top ? WideTop::bytes(h.k, plan.cta_n)
                              : h.teacher ? kHelpers * kSeenWords * 4 + kSlots * h.k * TeacherList::kBytes : 0;
     // chunks of four vectors a working thread, or a little more where that saves one
     const int parts = (plan.per_cta + kChunkVecs * 33 / 32 - 1) / (kChunkVecs * 33 / 32);
@@ -1410,17 +1574,41 @@ bool make_launch(const Shape& h, Launch& out) {
     return plan.chunks >= 2 && out.smem <= whole;
 }
 
+template <typename T, int OP, bool GRAD, bool ENT, bool TOP, int TEAM>
+cudaError_t launch_narrow(const RowArgs& a, cudaStream_t s) {
+    constexpr int kRows = kNarrowWarps / TEAM;
+    const int bytes = TOP ? NarrowTop::bytes(a.k, 1) : OP == OP_DISTILL ? kRows * (kSeenWords * 4 + a.k * TeacherList::kBytes) : 0;
+    static_assert(kNarrowWarps * (kSeenWords * 4 + TP_MAX_TEACHER_LOGITS * TeacherList::kBytes) + 1024 <= 48 * 1024);
+    narrow_kernel<T, OP, GRAD, ENT, TOP, TEAM><<<(unsigned)((a.n + (int64_t)kRows - 1) / kRows), kNarrowWarps * 32, bytes, s>>>(a);
+    return cudaGetLastError();
+}
+
 template <typename T, int OP, bool GRAD, bool ENT, bool TOP = false>
 cudaError_t launch_rows(const RowArgs& a, cudaStream_t s) {
     constexpr int E = Vec<T>::E;
+    if ((int64_t)a.vocab * (int)sizeof(T) <= kNarrowBytes) {
+        // one warp a row where it has at most four vectors for a lane and there are enough rows to fill the GPU
+        if constexpr (!TOP)
+            if (a.vocab * (int)sizeof(T) <= 2048 && a.n >= 2048) return launch_narrow<T, OP, GRAD, ENT, false, 1>(a, s);
+        return launch_narrow<T, OP, GRAD, ENT, TOP, kNarrowWarps>(a, s);
+    }
     // (rows that all begin in a line of their own have one vector less than rows at any place)
     const bool lines = (uintptr_t)a.x % 16 == 0 && (a.n == 1 || a.x_stride % E == 0);
     const Shape shape{a.n, (a.vocab + (lines ? 1 : 2) * (E - 1)) / E, a.k, (int)sizeof(RowShared<T>), GRAD, TOP, OP == OP_DISTILL};
     Launch l;
     if (!make_launch(shape, l)) return cudaErrorInvalidConfiguration;
     auto kernel = wide_kernel<T, OP, GRAD, ENT, TOP>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, l.smem);
+    // once a device: the largest size any call may ask for
+    static std::atomic<uint64_t> allowed{0};
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return e;
+    const uint64_t bit = 1ull << (device & 63);
+    if (device > 63 || !(allowed.load(std::memory_order_relaxed) & bit)) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxBytes - (int)sizeof(RowShared<T>));
+        if (e != cudaSuccess) return e;
+        allowed.fetch_or(bit, std::memory_order_relaxed);
+    }
     cudaLaunchAttribute attr[1] = {};
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = l.plan.cta_n;
