@@ -175,7 +175,12 @@ __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_
                  : "memory");
 }
 template <int THREADS>
-__device__ __forceinline__ void threads_sync() { asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory"); }
+__device__ __forceinline__ void threads_sync() {
+    if constexpr (THREADS == 32)
+        __syncwarp();
+    else
+        asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
+}
 __device__ __forceinline__ void row_threads_sync() { threads_sync<kRowThreads>(); }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
@@ -336,6 +341,9 @@ struct Row {
         for (int e = 0; e < E; ++e) f[e] = j0 + e >= 0 && j0 + e < vocab ? to_f32(x[j0 + e]) : kNegInf;
         return Vec<T>::pack(f);  // (exact: the values come from T)
     }
+    __device__ __forceinline__ uint4 load_kept(int v) const {
+        return whole(v) ? *(const uint4*)(x + (v * E - lead)) : load_part(v);
+    }
     __device__ __forceinline__ uint4 load(int v) const {
         return whole(v) ? __ldcs((const uint4*)(x + (v * E - lead))) : load_part(v);
     }
@@ -425,7 +433,7 @@ struct Running {
         m = base = m2;
     }
     template <typename T, bool ENT, int N>
-    __device__ __forceinline__ void add(const uint4* r, float c) {
+    __device__ __forceinline__ float add(const uint4* r, float c) {  // returns the largest of r
         const float m2 = Vec<T>::template max_of<N>(r);
         if (m2 > m) raise(m2, c);
         const F2 c2(c, c);
@@ -464,6 +472,7 @@ struct Running {
             }
             t = t + part;
         }
+        return m2;
     }
     __device__ __forceinline__ Stats stats() const {
         Stats r;
@@ -643,27 +652,29 @@ __device__ __forceinline__ float teacher_loss(const TeacherList& list, int k, co
 // Alternatives. A key holds a logit, in an order of unsigned integers, above the
 // complement of its id: the k largest keys are the k largest logits, of equal ones
 // the lower ids. Where k threads have met a logit of at least b, nothing below b is
-// among the slice's k. After the first chunk each warp takes the ceil(k / kWarps)-th
-// of its lanes' maxima and the CTA the least of these; from then on the threads
-// leave their maxima after every chunk, and the row's helper warp makes a higher b
-// of them as often as it can. What is not below b goes on the row's list. In the
-// end the helper leaves out what the last b excludes and ranks the rest by comparing
-// all with all, and one CTA's helper merges the cluster's. A list that overflows
-// (many equal logits, rows in rising order) is made again by finding the k-th
-// largest key by its digits.
+// among the k. So the pass that takes the statistics leaves each thread's largest
+// logit, of the whole slice and of each of up to kCells parts of it; b is about the
+// k-th largest of the former, and where a thread's largest of a part is not below b
+// (about k places) that thread's vectors of the part are read again, mostly from L2,
+// and what is not below b goes on a list: little more than k keys. One warp does all
+// this while the working warps are at the next rows, ranks the list by comparing all
+// with all, and one CTA's merges the cluster's. Where a list overflows (many equal
+// logits, rows in rising order) or too few threads have met any, it is made by
+// finding the k-th largest key by its digits.
+constexpr int kCells = 8;
+constexpr int kPlaces = 512;
 template <int THREADS, int SLOTS>
 struct TopShared {
     uint64_t best_full[SLOTS];
-    float most[SLOTS][THREADS];  // the threads' largest logits so far
-    float bound[SLOTS];          // what the helper has made of them
-    float first[2][THREADS / 32];
-    int n[SLOTS];
-    int digit, rest;
-    int hist[256];
+    float most[SLOTS][THREADS];                   // the threads' largest logits
+    __nv_bfloat16 part[SLOTS][kCells][THREADS];   // of the parts, rounded up
+    uint16_t place[SLOTS][kPlaces];               // thread and part that are read again
+    int n[SLOTS];                                 // keys on the list
+    int digit[SLOTS], rest[SLOTS], hist[SLOTS][256];
     // behind it: the slots' lists of list_size(k) keys, then the first CTA's best keys of each slot and CTA: k, descending,
     // 0 where none is left
 
-    static __host__ __device__ __forceinline__ int list_size(int k) { return 1024 + 8 * k; }
+    static __host__ __device__ __forceinline__ int list_size(int k) { return 4 * k + 64; }
     static __host__ __forceinline__ int bytes(int k, int cta_n) {
         return (int)sizeof(TopShared) + SLOTS * 8 * (list_size(k) + (cta_n > 1 ? cta_n * k : 0));
     }
@@ -744,37 +755,57 @@ __device__ __forceinline__ float warp_kth(float v, int at) {
     return __shfl_sync(0xffffffffu, v, at);
 }
 
-// Puts the logits of M vectors that are not below the bound on the list.
-template <typename T, int M>
-__device__ __forceinline__ void collect(const uint4* r, int v, int lead, float bound, Key* list, int size, int* n) {
+// Puts the logits of the vectors v, v + step, ... before end that are not below the bound on the list.
+template <typename T>
+__device__ __forceinline__ void collect(const Row<T>& row, int v, int end, int step, float bound, Key* list, int size, int* n) {
     constexpr int E = Vec<T>::E;
+    for (; v < end; v += 4 * step) {
+        uint4 r[4];
 #pragma unroll
-    for (int u = 0; u < M; ++u)
-        if (Vec<T>::template max_of<1>(r + u) >= bound) {
-            float x[E];
-            Vec<T>::unpack(r[u], x);
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (x[e] >= bound && x[e] > kNegInf) {
-                    const int at = atomicAdd(n, 1);
-                    if (at < size) list[at] = make_key(x[e], (v + u * kRowThreads) * E + e - lead);
-                }
+        for (int u = 0; u < 4; ++u) {
+            r[u] = make_uint4(Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone);
+            if (v + u * step < end) r[u] = row.load_kept(v + u * step);
         }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (Vec<T>::template max_of<1>(r + u) >= bound) {
+                float x[E];
+                Vec<T>::unpack(r[u], x);
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (x[e] >= bound && x[e] > kNegInf) {
+                        const int at = atomicAdd(n, 1);
+                        if (at < size) list[at] = make_key(x[e], (v + u * step) * E + e - row.lead);
+                    }
+            }
+    }
 }
 
-// The list of the slice's k largest keys, from memory; all working warps. The
-// k-th largest key is found by its digits of 8 bits, the highest first; the id's
-// highest digit is the same in all.
+// The list of the slice's k largest keys (it has more), from memory, by THREADS
+// threads. The k-th largest key is found by its digits of 8 bits, the highest first;
+// the id's highest digit is the same in all.
 template <int THREADS, typename T, typename S>
-__device__ __noinline__ void collect_exact(const Row<T>& row, int first, int n, int k, S& sh, Key* list, int* count) {
+__device__ __noinline__ void collect_exact(const Row<T>& row, int first, int n, int k, S& sh, int s) {
     constexpr int E = Vec<T>::E;
+    const int t = threadIdx.x % THREADS;
+    Key* list = sh.list(s, k);
+    int* hist = sh.hist[s];
     auto each_key = [&](auto f) {
-        for (int v = first + threadIdx.x; v < first + n; v += THREADS) {
-            float x[E];
-            Vec<T>::unpack(row.load(v), x);
+        for (int v = first + t; v < first + n; v += 4 * THREADS) {
+            uint4 r[4];
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (x[e] > kNegInf) f(make_key(x[e], v * E + e - row.lead));
+            for (int u = 0; u < 4; ++u) {
+                r[u] = make_uint4(Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone);
+                if (v + u * THREADS < first + n) r[u] = row.load_kept(v + u * THREADS);
+            }
+#pragma unroll 1
+            for (int u = 0; u < 4; ++u) {
+                float x[E];
+                Vec<T>::unpack(u == 0 ? r[0] : u == 1 ? r[1] : u == 2 ? r[2] : r[3], x);
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (x[e] > kNegInf) f(make_key(x[e], (v + u * THREADS) * E + e - row.lead));
+            }
         }
     };
     Key found = 0, mask = 0;
@@ -785,50 +816,50 @@ __device__ __noinline__ void collect_exact(const Row<T>& row, int first, int n, 
             mask |= (Key)0xff << 24;
             continue;
         }
-        for (int b = threadIdx.x; b < 256; b += THREADS) sh.hist[b] = 0;
+        for (int b = t; b < 256; b += THREADS) hist[b] = 0;
         threads_sync<THREADS>();
         each_key([&](Key key) {
-            if ((key & mask) == found) atomicAdd(&sh.hist[(int)(key >> shift) & 255], 1);
+            if ((key & mask) == found) atomicAdd(&hist[(int)(key >> shift) & 255], 1);
         });
         threads_sync<THREADS>();
-        if (threadIdx.x < 32) {  // lane l: digits 255 - 8 l downwards
+        if (t < 32) {  // lane l: digits 255 - 8 l downwards
             int sum = 0;
-            for (int b = 0; b < 8; ++b) sum += sh.hist[255 - 8 * threadIdx.x - b];
+            for (int b = 0; b < 8; ++b) sum += hist[255 - 8 * t - b];
             int before = sum;
             for (int off = 1; off < 32; off <<= 1) {
                 const int o = __shfl_up_sync(0xffffffffu, before, off);
-                if ((int)threadIdx.x >= off) before += o;
+                if (t >= off) before += o;
             }
-            if (threadIdx.x == 31) sh.digit = 0;  // (more keys than k: the list had overflowed)
+            if (t == 31) sh.digit[s] = 0, sh.rest[s] = 1;  // (one of the lanes below finds its digit: there are more than k keys)
             __syncwarp();
             before -= sum;
             if (before < rest && before + sum >= rest) {
-                int b = 0, own = sh.hist[255 - 8 * threadIdx.x];
+                int b = 0, own = hist[255 - 8 * t];
                 while (before + own < rest) {
                     before += own;
-                    own = sh.hist[255 - 8 * threadIdx.x - ++b];
+                    own = hist[255 - 8 * t - ++b];
                 }
-                sh.digit = 255 - 8 * threadIdx.x - b;
-                sh.rest = rest - before;
+                sh.digit[s] = 255 - 8 * t - b;
+                sh.rest[s] = rest - before;
             }
         }
         threads_sync<THREADS>();
-        found |= (Key)sh.digit << shift;
+        found |= (Key)sh.digit[s] << shift;
         mask |= (Key)0xff << shift;
-        rest = sh.rest;
+        rest = sh.rest[s];
     }
-    if (threadIdx.x == 0) *count = 0;
+    if (t == 0) sh.n[s] = 0;
     threads_sync<THREADS>();
     each_key([&](Key key) {
         if (key >= found) {
-            const int at = atomicAdd(count, 1);
-            list[at] = key;  // (k of them)
+            const int at = atomicAdd(&sh.n[s], 1);
+            if (at < S::list_size(k)) list[at] = key;  // (k of them)
         }
     });
     threads_sync<THREADS>();
 }
 
-// One helper warp: a value, at least b, that k of the threads' maxima are not below (b or -inf where there are fewer).
+// One warp: a value that k of the threads' maxima are not below, or b where that is larger (-inf: there is none).
 // Halving between the largest and b, in the order of keys, until at most k / 8 too many are left.
 template <int THREADS>
 __device__ __forceinline__ float kth_of_maxima(const float* most, int k, float b) {
@@ -836,7 +867,7 @@ __device__ __forceinline__ float kth_of_maxima(const float* most, int k, float b
     uint32_t v[THREADS / 32], lo = (uint32_t)(make_key(b, 0) >> 32), hi = lo;
 #pragma unroll
     for (int j = 0; j < THREADS / 32; ++j) {
-        v[j] = (uint32_t)(make_key(((volatile const float*)most)[lane + 32 * j], 0) >> 32);
+        v[j] = (uint32_t)(make_key(most[lane + 32 * j], 0) >> 32);
         hi = max(hi, v[j]);
     }
     hi = __reduce_max_sync(0xffffffffu, hi) + 1;
@@ -856,23 +887,39 @@ __device__ __forceinline__ float kth_of_maxima(const float* most, int k, float b
     return key_value((Key)lo << 32);
 }
 
-// One helper warp: the row's alternatives from the CTAs' lists. bound: nothing below it is one of them.
-template <int THREADS, typename S>
+// One helper warp: the list of what is not below the bound, from the working threads' parts of the slice.
+template <typename T>
+__device__ __forceinline__ void collect_parts(const Row<T>& row, int first, int n, int chunk, int k, float bound, WideTop& sh, int s) {
+    const int lane = threadIdx.x & 31, chunks = (n + chunk - 1) / chunk, per_part = (chunks + kCells - 1) / kCells;
+    Key* list = sh.list(s, k);
+    int m = 0;
+    for (int p = 0; p * per_part < chunks; ++p)
+        for (int t = lane; t < kRowThreads; t += 32) {
+            const float most = to_f32(sh.part[s][p][t]);
+            const bool hit = sh.most[s][t] >= bound && most >= bound && most > kNegInf;
+            const uint32_t hits = __ballot_sync(0xffffffffu, hit);
+            const int at = m + __popc(hits & ((1u << lane) - 1));
+            if (hit && at < kPlaces) sh.place[s][at] = (uint16_t)(p * kRowThreads + t);
+            m += __popc(hits);
+        }
+    __syncwarp();
+    if (m <= kPlaces)
+        for (int p = lane; p < m; p += 32) {  // a lane's loads are in flight with the others'
+            const int t = sh.place[s][p] % kRowThreads, u0 = sh.place[s][p] / kRowThreads * per_part;
+            for (int u = u0; u < min(u0 + per_part, chunks); ++u)
+                collect(row, first + u * chunk + t, first + min((u + 1) * chunk, n), kRowThreads, bound, list, WideTop::list_size(k), &sh.n[s]);
+        }
+    __syncwarp();
+    if (m > kPlaces || sh.n[s] > WideTop::list_size(k)) collect_exact<32>(row, first, n, k, sh, s);
+}
+
+// One helper warp: the row's alternatives from the CTAs' lists.
+template <typename S>
 __device__ __forceinline__ void alternatives(const RowArgs& a, int64_t i, S& sh, int s, uint32_t parity, uint32_t rank, int cta_n,
-                                             float bound, const RowResult& r, volatile int* dead) {
+                                             const RowResult& r, volatile int* dead) {
     const int lane = threadIdx.x & 31, k = a.k;
     Key* list = sh.list(s, k);
-    const int met = min(sh.n[s], S::list_size(k));
-    if (met > 2 * k + 32) bound = fmaxf(bound, kth_of_maxima<THREADS>(sh.most[s], k, bound));
-    const Key least = bound > kNegInf ? make_key(bound, 0x7fffffff) : 0;  // of its equals the last
-    int m = 0;
-    for (int p0 = 0; p0 < met; p0 += 32) {  // left out in place: never written ahead of what is read
-        const Key key = p0 + lane < met ? list[p0 + lane] : 0;
-        const uint32_t stays = __ballot_sync(0xffffffffu, key >= least && key != 0);
-        if (stays >> lane & 1) list[m + __popc(stays & ((1u << lane) - 1))] = key;
-        m += __popc(stays);
-        __syncwarp();
-    }
+    const int m = min(sh.n[s], S::list_size(k));
     const bool nan = isnan(r.lse), alone = cta_n == 1;
     auto write = [&](int place, Key key) {
         const bool some = key != 0 && !nan;
@@ -897,28 +944,43 @@ __device__ __forceinline__ void alternatives(const RowArgs& a, int64_t i, S& sh,
     }
     if (alone || rank != 0) return;
     mbar_wait(smem_addr(&sh.best_full[s]), parity, dead);
+    // of two descending lists the larger of A_i and B_(P - 1 - i) are the P largest, in an order that log2(P) rounds of
+    // exchanges sort; place p is lane p % 32's, its (p / 32)-th
+    constexpr int kMost = TP_MAX_ALTERNATIVES / 32;
     const Key* best = sh.best(s, 0, k, cta_n);
-    int top = 1;
-    while (2 * top <= k) top *= 2;
-    for (int p = lane; p < cta_n * k; p += 32) {
-        const int own = p / k;
-        const Key key = best[p];
-        // how many of each CTA's come before: larger, or for "none" (0) the lower CTA's; the searches side by side
-        int before[kMaxCluster] = {};
-        for (int step = top; step; step /= 2)
+    const int regs = k <= 32 ? 1 : k <= 64 ? 2 : 4, P = 32 * regs;
+    Key x[kMost];
 #pragma unroll
-            for (int q = 0; q < kMaxCluster; ++q) {
-                const int at = before[q] + step;
-                if (q >= cta_n || at > k) continue;
-                const Key o = best[q * k + at - 1];
-                if (o > key || (o == key && q < own)) before[q] = at;
+    for (int j = 0; j < kMost; ++j) x[j] = 32 * j + lane < k ? best[32 * j + lane] : 0;
+    for (int q = 1; q < cta_n; ++q) {
+#pragma unroll
+        for (int j = 0; j < kMost; ++j)
+            if (j < regs) {
+                const int at = P - 1 - (32 * j + lane);
+                const Key y = at < k ? best[q * k + at] : 0;
+                x[j] = max(x[j], y);
             }
-        int place = p - own * k;
 #pragma unroll
-        for (int q = 0; q < kMaxCluster; ++q)
-            if (q != own) place += before[q];
-        if (place < k) write(place, key);
+        for (int step = kMost / 2; step; step /= 2)  // between a lane's own
+            if (step < regs)
+#pragma unroll
+                for (int j = 0; j < kMost; ++j)
+                    if (!(j & step) && j + step < kMost) {
+                        const Key u = max(x[j], x[j + step]), w = min(x[j], x[j + step]);
+                        x[j] = u, x[j + step] = w;
+                    }
+#pragma unroll
+        for (int step = 16; step; step /= 2)
+#pragma unroll
+            for (int j = 0; j < kMost; ++j)
+                if (j < regs) {
+                    const Key o = __shfl_xor_sync(0xffffffffu, x[j], step);
+                    x[j] = lane & step ? min(x[j], o) : max(x[j], o);
+                }
     }
+#pragma unroll
+    for (int j = 0; j < kMost; ++j)
+        if (32 * j + lane < k) write(32 * j + lane, x[j]);
 }
 
 // ----------------------------------------------------------- helper warps --
@@ -1092,22 +1154,10 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
                     info.old = old;
                 }
             }
-            if constexpr (TOP) {
-                for (int k = lane; k < kRowThreads; k += 32) sh.most[s][k] = kNegInf;
-                if (lane == 0) sh.bound[s] = kNegInf, sh.n[s] = 0;
-            }
+            if (TOP && lane == 0) sh.n[s] = 0;
             __syncwarp();
             if (lane == 0) mbar_arrive(info_full + 8 * s);
             look(q + kSlots);
-            if constexpr (TOP) {
-                float b = kNegInf;
-                while (plan.per_cta > plan.chunk && !mbar_try(parts_full + 8 * s, parity_of(q)) && !*(volatile int*)&sm.dead) {
-                    b = kth_of_maxima<kRowThreads>(sh.most[s], a.k, b);
-                    if (lane == 0) *(volatile float*)&sh.bound[s] = b;
-                    __syncwarp();
-                }
-            }
-
             // ---- the row's results, from all parts in the same order
             mbar_wait_idle(parts_full + 8 * s, parity_of(q), &sm.dead);
             Stats all;
@@ -1133,12 +1183,16 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
             all.s = warp_sum(all.s);
             if (ENT) all.t = warp_sum(all.t);
             if (*(volatile int*)&sm.dead) all.s = NAN;
-            if constexpr (TOP) {  // the largest of the CTAs' bounds (none: -inf, their lists are exact)
-                bound = kNegInf;
+            if constexpr (TOP) {
+                // the largest over the CTAs of the least over their warps, or a better one from this CTA's threads
 #pragma unroll
-                for (int k = 0; k < kMost; ++k)
-                    if (p[k].w < INFINITY) bound = fmaxf(bound, p[k].w);
-                bound = warp_max(bound);
+                for (int k = 0; k < kMost; ++k) {
+                    float least = lane + 32 * k < cta_n * kWarps ? p[k].w : kNegInf;
+#pragma unroll
+                    for (int off = 1; off < kWarps; off *= 2) least = fminf(least, __shfl_xor_sync(0xffffffffu, least, off));
+                    bound = fmaxf(bound, least);
+                }
+                bound = kth_of_maxima<kRowThreads>(sh.most[s], a.k, warp_max(bound));
             }
             const RowResult res(all, c, inv_t);
             const bool live = info.live;
@@ -1149,7 +1203,10 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
                 mbar_arrive(coef_full + 8 * s);
                 if (rank == 0) write_results<OP, ENT>(a, i, live, info.w, res, logp, term);
             }
-            if constexpr (TOP) alternatives<kRowThreads>(a, i, sh, s, parity_of(q), rank, cta_n, bound, res, &sm.dead);
+            if constexpr (TOP) {
+                if (live) collect_parts(row, first, max(0, min(plan.per_cta, row.n_vec - first)), plan.chunk, a.k, bound, sh, s);
+                alternatives(a, i, sh, s, parity_of(q), rank, cta_n, res, &sm.dead);
+            }
             if (OP == OP_DISTILL && rank == 0) {
                 const float loss = live && !info.bad ? teacher_loss(list_at(s), a.k, res) : 0.f;
                 if (lane == 0) a.loss[i] = !live ? 0.f : info.bad || isnan(res.lse) ? NAN : info.w * loss;
@@ -1181,7 +1238,7 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
                         if (v1 > v0 && !*(volatile int*)&sm.dead) {
                             mbar_expect(full + 8 * slot, (v1 - v0) * 16);
                             bulk_copy(smem_addr(ring) + slot * slot_bytes + (v0 - v) * 16, row.x + ((int64_t)v0 * E - row.lead),
-                                      (v1 - v0) * 16, full + 8 * slot, GRAD && pass == 0 ? keep_in_l2() : pass_l2());
+                                      (v1 - v0) * 16, full + 8 * slot, (GRAD || TOP) && pass == 0 ? keep_in_l2() : pass_l2());
                         } else {
                             mbar_arrive(full + 8 * slot);
                         }
@@ -1208,56 +1265,36 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
             const int s = slot_of(q);
             mbar_wait(info_full + 8 * s, parity_of(q), &sm.dead);
             Running run;
-            float bound = INFINITY;  // TOP: the alternatives', while there is none
+            float bound = kNegInf;
             if (sm.info[s].live) {
                 const Row<T>& row = sm.info[s].row;
                 const Slice<T> slice = slice_at(row.n_vec);
                 const int chunks = slice.chunks();
+                const int per_part = (chunks + kCells - 1) / kCells;
+                float part = kNegInf;
                 for (int k = 0; k < chunks; ++k) {
                     const uint8_t* data = chunk_here();
-                    if constexpr (TOP) {
-                        const int lead = row.lead, size = WideTop::list_size(a.k);
-                        Key* list = sh.list(s, a.k);
-                        slice.template each<4>(data, k, [&](auto count, const uint4* r, int v, bool) {
-                            run.add<T, ENT, decltype(count)::n>(r, c);
-                            if (k > 0) collect<T, decltype(count)::n>(r, v, lead, bound, list, size, &sh.n[s]);
-                        });
-                        *(volatile float*)&sh.most[s][tid] = run.m;
-                        if (k == 0) {
-                            float* firsts = sh.first[q & 1];
-                            const float own = warp_kth(run.m, (a.k + kWarps - 1) / kWarps - 1);
-                            if (lane == 0) firsts[warp] = own;
-                            row_threads_sync();
-                            bound = firsts[lane % kWarps];
-#pragma unroll
-                            for (int off = 16; off; off >>= 1) bound = fminf(bound, __shfl_xor_sync(0xffffffffu, bound, off));
-                            slice.template each<1>(data, 0, [&](Count<1>, const uint4* r, int v, bool) {
-                                collect<T, 1>(r, v, lead, bound, list, size, &sh.n[s]);
-                            });
-                        } else {
-                            bound = fmaxf(bound, *(volatile float*)&sh.bound[s]);
-                        }
-                    } else {
-                        slice.template each<4>(data, k, [&](auto count, const uint4* r, int, bool) {
-                            run.add<T, ENT, decltype(count)::n>(r, c);
-                        });
-                    }
+                    slice.template each<4>(data, k, [&](auto count, const uint4* r, int, bool) {
+                        const float m2 = run.add<T, ENT, decltype(count)::n>(r, c);
+                        if (TOP) part = fmaxf(part, m2);
+                    });
                     chunk_done();
-                }
-                if constexpr (TOP) {
-                    row_threads_sync();
-                    if (sh.n[s] > WideTop::list_size(a.k)) {
-                        row_threads_sync();
-                        collect_exact<kRowThreads>(row, first, slice.n, a.k, sh, sh.list(s, a.k), &sh.n[s]);
-                        bound = kNegInf;
+                    if (TOP && ((k + 1) % per_part == 0 || k + 1 == chunks)) {
+                        sh.part[s][k / per_part][tid] = __float2bfloat16_ru(part);
+                        part = kNegInf;
                     }
                 }
+            }
+            if constexpr (TOP) {  // and this warp's ceil(k / kWarps)-th largest
+                sh.most[s][tid] = run.m;
+                bound = warp_kth(run.m, (a.k + kWarps - 1) / kWarps - 1);
             }
             Stats st = run.stats();
             st.join_warp<ENT>(c);
             const bool low = GRAD && ENT && __any_sync(0xffffffffu, run.low);
             // (a gradient waits for its row's, see there: no CTA of the cluster is more than three rows ahead of a helper)
             if (!GRAD && q >= 2) mbar_wait(coef_full + 8 * slot_of(q - 2), parity_of(q - 2), &sm.dead);
+            if (TOP) row_threads_sync();  // (the helper reads what all threads left)
             if (tid == 0) mbar_expect(parts_full + 8 * s, cta_n * kWarps * 16);
             if (lane < cta_n)
                 send(map_to(smem_addr(&sm.parts[s][rank][warp]), lane), map_to(parts_full + 8 * s, lane), st.m, st.s, st.t,
@@ -1332,7 +1369,7 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
 // comes from L1 or L2. What a row costs in wide_kernel beside its elements (about
 // 1 us of a CTA: helpers, barriers, exchange) would be most of a short row's time.
 constexpr int kNarrowWarps = 4;
-constexpr int kNarrowBytes = 16384;
+constexpr int kNarrowBytes = 32768;
 typedef TopShared<kNarrowWarps * 32, 1> NarrowTop;
 
 template <typename T, int OP, bool GRAD, bool ENT, bool TOP, int TEAM>
@@ -1386,13 +1423,13 @@ __global__ void __launch_bounds__(kNarrowWarps * 32) narrow_kernel(const __grid_
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 r[u] = make_uint4(Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone);
-                if (g + u * kTeam + lane < row.n_vec) r[u] = row.load(g + u * kTeam + lane);
+                if (g + u * kTeam + lane < row.n_vec) r[u] = row.load_kept(g + u * kTeam + lane);
             }
             f(Count<4>{}, r, g + lane);
         }
         for (; g < row.n_vec; g += kTeam) {
             uint4 r = make_uint4(Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone);
-            if (g + lane < row.n_vec) r = row.load(g + lane);
+            if (g + lane < row.n_vec) r = row.load_kept(g + lane);
             f(Count<1>{}, &r, g + lane);
         }
     };
@@ -1436,24 +1473,17 @@ __global__ void __launch_bounds__(kNarrowWarps * 32) narrow_kernel(const __grid_
     }
     if constexpr (TOP) {
         Key* keys = sh.list(0, a.k);
-        float bound = kNegInf;
         if (live) {
-            bound = kth_of_maxima<kTeam>(sh.most[0], a.k, kNegInf);
-            // (a longer list takes longer to rank than to make exactly)
-            const int size = min(4 * a.k + 64, NarrowTop::list_size(a.k));
-            each([&](auto count, const uint4* r, int v) {
-#pragma unroll
-                for (int u = 0; u < decltype(count)::n; ++u)
-                    collect<T, 1>(r + u, v + u * kTeam, row.lead, bound, keys, size, &sh.n[0]);
-            });
+            const float bound = kth_of_maxima<kTeam>(sh.most[0], a.k, kNegInf);
+            const int size = NarrowTop::list_size(a.k);
+            if (run.m >= bound) collect(row, t, row.n_vec, kTeam, bound, keys, size, &sh.n[0]);
             sync();
             if (sh.n[0] > size) {
                 sync();
-                collect_exact<kTeam>(row, 0, row.n_vec, a.k, sh, keys, &sh.n[0]);
-                bound = kNegInf;
+                collect_exact<kTeam>(row, 0, row.n_vec, a.k, sh, 0);
             }
         }
-        if (warp == 0) alternatives<kTeam>(a, i, sh, 0, 0, 0, 1, bound, res, nullptr);
+        if (warp == 0) alternatives(a, i, sh, 0, 0, 0, 1, res, nullptr);
     }
 }
 
@@ -1527,6 +1557,8 @@ cudaError_t by_type(const RowArgs& a, F f) {
 }
 
 constexpr int kMaxBytes = 232448;  // of shared memory a CTA
+template <typename T>
+constexpr int kFixedBytes = ((int)sizeof(RowShared<T>) + 255) / 256 * 256;  // the static part of it, with the compiler's padding
 
 // The cluster and ring of a call.
 struct Shape {
@@ -1594,7 +1626,7 @@ cudaError_t launch_rows(const RowArgs& a, cudaStream_t s) {
     }
     // (rows that all begin in a line of their own have one vector less than rows at any place)
     const bool lines = (uintptr_t)a.x % 16 == 0 && (a.n == 1 || a.x_stride % E == 0);
-    const Shape shape{a.n, (a.vocab + (lines ? 1 : 2) * (E - 1)) / E, a.k, (int)sizeof(RowShared<T>), GRAD, TOP, OP == OP_DISTILL};
+    const Shape shape{a.n, (a.vocab + (lines ? 1 : 2) * (E - 1)) / E, a.k, kFixedBytes<T>, GRAD, TOP, OP == OP_DISTILL};
     Launch l;
     if (!make_launch(shape, l)) return cudaErrorInvalidConfiguration;
     auto kernel = wide_kernel<T, OP, GRAD, ENT, TOP>;
@@ -1605,7 +1637,7 @@ cudaError_t launch_rows(const RowArgs& a, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     const uint64_t bit = 1ull << (device & 63);
     if (device > 63 || !(allowed.load(std::memory_order_relaxed) & bit)) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxBytes - (int)sizeof(RowShared<T>));
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxBytes - kFixedBytes<T>);
         if (e != cudaSuccess) return e;
         allowed.fetch_or(bit, std::memory_order_relaxed);
     }
