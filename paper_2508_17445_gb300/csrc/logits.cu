@@ -28,6 +28,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <utility>
 
 #include "logits.h"
 
@@ -90,6 +91,13 @@ __device__ __forceinline__ F2 exp2_of(F2 x) {
     float a, b;
     x.get(a, b);
     return F2(exp2_approx(a), exp2_approx(b));
+}
+
+// Launched while the predecessor on the stream may still run: it is waited for
+// before anything is read or written, and the successor may be launched likewise.
+__device__ __forceinline__ void after_predecessor() {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -998,39 +1006,54 @@ __device__ __forceinline__ void keep_edge(RowInfo<T>& info, T x) {
     if (e < Vec<T>::E) ((T*)&info.edge[lane / 16])[e] = x;
 }
 
-// The teacher's shares of one row of a distillation.
+// A teacher's answer to one row of a distillation, by one warp: whether there is one, and ...
+struct Teacher {
+    float best;
+    bool bad, live;  // bad: NaN or +inf in it
+};
+__device__ __forceinline__ Teacher teacher_first(const RowArgs& a, int64_t i) {
+    const int lane = threadIdx.x & 31;
+    Teacher t;
+    t.best = kNegInf;
+    t.bad = false;
+#pragma unroll 4
+    for (int k = lane; k < a.k; k += 32) {
+        const int32_t id = a.teacher_ids[i * a.k + k];
+        const float v = load_value(a.teacher_logits, i * a.k + k, a.teacher_dtype);
+        if (id >= 0) {
+            t.bad |= isnan(v) || v == INFINITY;
+            t.best = fmaxf(t.best, v);
+        }
+    }
+    t.best = warp_max(t.best);
+    t.bad = __any_sync(0xffffffffu, t.bad);
+    t.live = t.bad || t.best > kNegInf;
+    return t;
+}
+
+// ... its shares, with what the slice's part of the gradient and (the first CTA) the loss take.
 template <typename T>
-__device__ __forceinline__ void teacher_ahead(const RowArgs& a, int64_t i, const Row<T>& row, int first, int n, uint32_t rank,
-                                              RowInfo<T>& info, const TeacherList& list, uint32_t* seen) {
+__device__ __forceinline__ void teacher_rest(const RowArgs& a, int64_t i, const Teacher& t, const Row<T>& row, int first, int n,
+                                             uint32_t rank, RowInfo<T>& info, const TeacherList& list, uint32_t* seen) {
     const int lane = threadIdx.x & 31;
     const float c = kLog2e / a.temperature;
     const int32_t* ids = a.teacher_ids + i * a.k;
-    float best = kNegInf;
-    bool bad = false;
-    for (int k = lane; k < a.k; k += 32)
-        if (ids[k] >= 0) {
-            const float v = load_value(a.teacher_logits, i * a.k + k, a.teacher_dtype);
-            bad |= isnan(v) || v == INFINITY;
-            best = fmaxf(best, v);
-        }
-    best = warp_max(best);
-    bad = __any_sync(0xffffffffu, bad);
-    const bool live = bad || best > kNegInf;
+    auto weight = [&](int k) { return exp2_approx(c * (load_value(a.teacher_logits, i * a.k + k, a.teacher_dtype) - t.best)); };
     bool off = false, twice = false;
     int n_own = 0;
-    if (live && !bad) {
+    if (t.live && !t.bad) {
         float sum = 0.f;
-        for (int k = lane; k < a.k; k += 32)
-            if (ids[k] >= 0) sum += exp2_approx(c * (load_value(a.teacher_logits, i * a.k + k, a.teacher_dtype) - best));
+#pragma unroll 4
+        for (int k = lane; k < a.k; k += 32) sum += ids[k] >= 0 ? weight(k) : 0.f;
         sum = warp_sum(sum);
         const int lo = first * Row<T>::E - row.lead, hi = lo + n * Row<T>::E;
+#pragma unroll 2
         for (int k0 = 0; k0 < a.k; k0 += 32) {
             const int k = k0 + lane;
             int32_t id = -1;
-            float q = 0.f;
             if (k < a.k) {
                 id = ids[k];
-                if (id >= 0) q = exp2_approx(c * (load_value(a.teacher_logits, i * a.k + k, a.teacher_dtype) - best)) / sum;
+                const float q = id >= 0 ? weight(k) / sum : 0.f;
                 if (!(q > 0.f)) id = -1;
                 off |= id >= row.vocab;
                 const bool own = id >= 0 && id < row.vocab && id >= lo && id < hi;
@@ -1053,12 +1076,12 @@ __device__ __forceinline__ void teacher_ahead(const RowArgs& a, int64_t i, const
         twice = __any_sync(0xffffffffu, twice);
     }
     if (lane == 0) {
-        info.live = live;
-        info.bad = bad || off;
+        info.bad = t.bad || off;
         info.n_own = n_own;
         info.repeats = twice;
         info.w = a.weight ? a.weight[i] : 1.f;
     }
+    __syncwarp();
 }
 
 // GRAD: a gradient is asked for. ENT: the entropy is (or is in the gradient). TOP: alternatives.
@@ -1107,6 +1130,7 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
     __syncthreads();
     cluster_arrive();  // every CTA's barriers are there
     cluster_wait();
+    after_predecessor();
 
     if (warp > kCopyWarp) {
         // ---- helper s: rows s, s + kSlots, ...
@@ -1141,22 +1165,32 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
             if (OP == OP_DISTILL) edge = edge_element(row, first, plan.per_cta);
             mbar_wait_idle(info_empty + 8 * s, parity_of(q) ^ 1, &sm.dead);
             keep_edge(info, edge);
-            if constexpr (OP == OP_DISTILL)
-                teacher_ahead(a, i, row, first, max(0, min(plan.per_cta, row.n_vec - first)), rank, info, list_at(s), seen + s * kSeenWords);
-            if (lane == 0) {
-                info.row = row;
-                if (OP != OP_DISTILL) {
+            Teacher teacher{};
+            if constexpr (OP == OP_DISTILL) teacher = teacher_first(a, i);
+            auto own_values = [&] {  // what nobody reads before the coefficients
+                if constexpr (OP == OP_DISTILL) {
+                    teacher_rest(a, i, teacher, row, first, max(0, min(plan.per_cta, row.n_vec - first)), rank, info, list_at(s),
+                                 seen + s * kSeenWords);
+                } else if (lane == 0) {
                     info.tok = tok;
-                    info.live = tok >= 0;
                     info.x_tok = x_tok;
                     info.w = w;
                     info.adv = adv;
                     info.old = old;
                 }
+            };
+            if (lane == 0) {
+                info.row = row;
+                info.live = OP == OP_DISTILL ? teacher.live : tok >= 0;
             }
             if (TOP && lane == 0) sh.n[s] = 0;
+            // a gradient in place may overwrite, in another CTA, what is read here once this CTA's statistics are sent
+            const bool in_place = GRAD && a.dx == a.x;
+            if (in_place) own_values();
             __syncwarp();
             if (lane == 0) mbar_arrive(info_full + 8 * s);
+            if (!in_place) own_values();
+            __syncwarp();
             look(q + kSlots);
             // ---- the row's results, from all parts in the same order
             mbar_wait_idle(parts_full + 8 * s, parity_of(q), &sm.dead);
@@ -1381,6 +1415,7 @@ __global__ void __launch_bounds__(kNarrowWarps * 32) narrow_kernel(const __grid_
     __shared__ float4 parts[kNarrowWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, team = warp / TEAM, t = threadIdx.x - team * kTeam;
     const int64_t i = (int64_t)blockIdx.x * kRows + team;
+    after_predecessor();
     if (i >= a.n) return;  // (a whole warp, and with one row a CTA none)
     auto sync = [] {
         if constexpr (TEAM == 1)
@@ -1399,7 +1434,9 @@ __global__ void __launch_bounds__(kNarrowWarps * 32) narrow_kernel(const __grid_
         if (t < 32) {
             for (int k = lane; k < kSeenWords; k += 32) seen[k] = 0;
             __syncwarp();
-            teacher_ahead(a, i, row, 0, row.n_vec, 0, info, list, seen);
+            const Teacher teacher = teacher_first(a, i);
+            if (lane == 0) info.live = teacher.live;
+            teacher_rest(a, i, teacher, row, 0, row.n_vec, 0, info, list, seen);
         }
     } else if (t == 0) {
         const int32_t tok = a.tokens ? a.tokens[i] : 0;
@@ -1497,6 +1534,7 @@ __global__ void __launch_bounds__(kBackThreads) backward_kernel(const RowArgs a,
     const int64_t i = blockIdx.x / ctas_per_row;
     const int first = (int)(blockIdx.x % ctas_per_row) * kBackThreads * kBackVecs + threadIdx.x;
     const Row<T> row(a, i);
+    after_predecessor();
     const int32_t tok = a.tokens ? a.tokens[i] : 0;
     if (tok < 0) {
         const uint4 zero = make_uint4(0, 0, 0, 0);
@@ -1549,6 +1587,24 @@ __global__ void __launch_bounds__(kBackThreads) backward_kernel(const RowArgs a,
 }
 
 // ---------------------------------------------------------------- launches --
+template <typename... P, typename... A>
+cudaError_t launch_kernel(void (*kernel)(P...), int64_t ctas, int cluster, int threads, int smem, cudaStream_t s, A&&... args) {
+    cudaLaunchAttribute attr[2] = {};
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 0 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...);
+}
+
 template <typename F>
 cudaError_t by_type(const RowArgs& a, F f) {
     if (a.dtype == TP_F32) return f(float{});
@@ -1572,12 +1628,12 @@ struct Launch {
 };
 
 // Two CTAs share an SM, so that one works while the other waits. Fewer CTAs a row
-// exchange less, but a gradient's rows at work have to stay in L2 together with what
-// is written meanwhile: at most kRowsInL2 of them. Few rows are spread over more
-// CTAs, down to slices of 8 KB. Long lists of alternatives leave room for one CTA an
-// SM only. False: too large.
+// exchange less; more of them end together where the rows do not fill the last round,
+// and a gradient's rows at work have to stay in L2 together with what is written
+// meanwhile: at most kRowsInL2 of them. Slices below 8 KB are not cut further. Long
+// lists of alternatives leave room for one CTA an SM only. False: too large.
 bool make_launch(const Shape& h, Launch& out) {
-    constexpr int kSms = 152, kSmBytes = 233472, kReserved = 1024;
+    constexpr int kSmBytes = 233472, kReserved = 1024;
     constexpr int64_t kRowsInL2 = 48ll << 20;
     constexpr int kChunkVecs = 4 * kRowThreads, kAtLeast = 3 * kChunkVecs * 16;  // of a ring
     // clusters of 1, 2, 4 and 8 CTAs that the GPU holds at once, one or two CTAs an SM
@@ -1585,11 +1641,15 @@ bool make_launch(const Shape& h, Launch& out) {
     const int half = kSmBytes / 2 - kReserved - h.fixed, whole = kMaxBytes - h.fixed;
     Plan& plan = out.plan;
     int size = 0;  // log2 of the CTAs a row
-    for (; size < 3; ++size) {
-        const int64_t slice = (int64_t)(h.n_vec + (1 << size) - 1) / (1 << size) * 16;
-        const bool spread = (int64_t)h.n * 2 << size <= kSms && slice > 8192;
-        const bool far = h.grad && (int64_t)std::min(h.n, kClusters[1][size]) * h.n_vec * 16 > kRowsInL2;
-        if (!spread && !far) break;
+    float least = INFINITY;
+    for (int k = 0; k < 4; ++k) {
+        const int64_t slice = (int64_t)(h.n_vec + (1 << k) - 1) / (1 << k) * 16;
+        const int64_t at_work = std::min(h.n, kClusters[1][k]);
+        if (k < 3 && h.grad && at_work * h.n_vec * 16 > kRowsInL2) continue;
+        const float row = (float)slice * (h.grad ? 2 : 1) / 22.4e3f + 0.6f + 0.3f * k;  // us: a CTA's share of HBM, and once a row
+        const float cost = row * (float)((h.n + at_work - 1) / at_work);
+        if (k > 0 && slice < 8192) break;
+        if (cost < least) least = cost, size = k;
     }
     plan.cta_n = 1 << size;
     plan.per_cta = (h.n_vec + plan.cta_n - 1) / plan.cta_n;
@@ -1611,8 +1671,7 @@ cudaError_t launch_narrow(const RowArgs& a, cudaStream_t s) {
     constexpr int kRows = kNarrowWarps / TEAM;
     const int bytes = TOP ? NarrowTop::bytes(a.k, 1) : OP == OP_DISTILL ? kRows * (kSeenWords * 4 + a.k * TeacherList::kBytes) : 0;
     static_assert(kNarrowWarps * (kSeenWords * 4 + TP_MAX_TEACHER_LOGITS * TeacherList::kBytes) + 1024 <= 48 * 1024);
-    narrow_kernel<T, OP, GRAD, ENT, TOP, TEAM><<<(unsigned)((a.n + (int64_t)kRows - 1) / kRows), kNarrowWarps * 32, bytes, s>>>(a);
-    return cudaGetLastError();
+    return launch_kernel(narrow_kernel<T, OP, GRAD, ENT, TOP, TEAM>, (a.n + (int64_t)kRows - 1) / kRows, 0, kNarrowWarps * 32, bytes, s, a);
 }
 
 template <typename T, int OP, bool GRAD, bool ENT, bool TOP = false>
@@ -1641,26 +1700,14 @@ cudaError_t launch_rows(const RowArgs& a, cudaStream_t s) {
         if (e != cudaSuccess) return e;
         allowed.fetch_or(bit, std::memory_order_relaxed);
     }
-    cudaLaunchAttribute attr[1] = {};
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = l.plan.cta_n;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(l.clusters * l.plan.cta_n));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = (size_t)l.smem;
-    cfg.stream = s;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, a, l.plan);
+    return launch_kernel(kernel, (int64_t)l.clusters * l.plan.cta_n, l.plan.cta_n, kThreads, l.smem, s, a, l.plan);
 }
 
 template <typename T, bool ENT>
 cudaError_t launch_back(const RowArgs& a, cudaStream_t s) {
     constexpr int E = Vec<T>::E, per_cta = kBackThreads * kBackVecs;
     const int ctas = ((a.vocab + 2 * E - 2) / E + per_cta - 1) / per_cta;
-    backward_kernel<T, ENT><<<(unsigned)(a.n * ctas), kBackThreads, 0, s>>>(a, ctas);
-    return cudaGetLastError();
+    return launch_kernel(backward_kernel<T, ENT>, (int64_t)a.n * ctas, 0, kBackThreads, 0, s, a, ctas);
 }
 
 }  // namespace
