@@ -26,6 +26,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <limits.h>
+
 #include <algorithm>
 #include <atomic>
 #include <utility>
@@ -43,6 +45,7 @@ constexpr int kThreads = (kWarps + 1 + kHelpers) * 32;
 constexpr int kRowThreads = kWarps * 32;
 constexpr int kSlots = 4;            // rows whose values and statistics are held at once
 constexpr int kMaxChunks = 32;       // of the ring
+constexpr int kClaims = 2 * kSlots;  // rows taken over whose numbers are held
 constexpr uint64_t kWaitLimitNs = 2000000000ull;  // bounded waits: 2 s
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -107,6 +110,33 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
+// Takes over a cluster of this grid that has not been launched yet: 16 bytes at `at`
+// (in every CTA of this cluster, at the same place), counted by the barrier `bar`,
+// say which, or that there is none left.
+__device__ __forceinline__ void claim_cluster(uint32_t at, uint32_t bar, bool alone) {
+    if (alone)
+        asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(at), "r"(bar)
+                     : "memory");
+    else
+        asm volatile(
+            "clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.multicast::cluster::all.b128 [%0], [%1];" ::"r"(at),
+            "r"(bar)
+            : "memory");
+}
+// The first CTA of the cluster that was taken over, -1: none was.
+__device__ __forceinline__ int claimed_cta(uint32_t at) {
+    uint32_t ok, x;
+    asm volatile(
+        "{ .reg .pred p; .reg .b128 r; ld.shared.b128 r, [%2];\n"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r; selp.u32 %0, 1, 0, p; mov.u32 %1, 0;\n"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r; }"
+        : "=&r"(ok), "=&r"(x)
+        : "r"(at)
+        : "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before the place is written to again
+    return ok ? (int)x : -1;
+}
+
 // The address in CTA `rank` of the cluster of what is at `addr` here.
 __device__ __forceinline__ uint32_t map_to(uint32_t addr, uint32_t rank) {
     uint32_t r;
@@ -531,6 +561,7 @@ template <typename T>
 struct RowInfo {
     Row<T> row;
     uint4 edge[2];      // the slice's vectors that the row shares with its neighbours, the first and the last
+    int32_t end;        // there is no such row, nor any after it
     int32_t live, tok;  // not live: padding
     float x_tok, w, adv, old;
     int32_t bad, n_own; // distillation: the teacher's answer is not one; its tokens in this CTA's slice
@@ -551,6 +582,9 @@ struct RowShared {
     Coef coef[kSlots];
     uint64_t full[kMaxChunks], empty[kMaxChunks];                                           // of the ring's chunks
     uint64_t info_full[kSlots], info_empty[kSlots], parts_full[kSlots], coef_full[kSlots];  // of a row's slot
+    uint4 claim[kClaims];
+    uint64_t claim_full[kClaims];
+    int last;  // the cluster's rows, once that is known
     int dead;
 };
 
@@ -697,10 +731,11 @@ struct Plan {
     int cta_n;          // CTAs a cluster
     int chunk, chunks;  // vectors a chunk, chunks of the ring
     int per_cta;        // vectors a slice
+    int claims;         // rows are taken over from clusters not yet launched (a cluster a row in the grid)
 };
 
-// A row's slice as the working warps see it: groups of 32 vectors, group g of a
-// chunk is warp (g % kWarps)'s.
+// A row's slice as the working warps see it: groups of 32 vectors, group g of chunk
+// k is warp ((g - k) % kWarps)'s, so that no warp has the odd groups of all chunks.
 template <int N>
 struct Count {
     static constexpr int n = N;
@@ -717,7 +752,7 @@ struct Slice {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         const uint4* data = (const uint4*)at + lane;
         const int m = min(chunk, n - k * chunk), v = first + k * chunk + lane;
-        int g = warp * 32;
+        int g = (warp + k) % kWarps * 32;
         auto some = [&](auto count) {
             constexpr int M = decltype(count)::n;
             uint4 r[M];
@@ -915,7 +950,8 @@ __device__ __forceinline__ void collect_parts(const Row<T>& row, int first, int 
         for (int p = lane; p < m; p += 32) {  // a lane's loads are in flight with the others'
             const int t = sh.place[s][p] % kRowThreads, u0 = sh.place[s][p] / kRowThreads * per_part;
             for (int u = u0; u < min(u0 + per_part, chunks); ++u)
-                collect(row, first + u * chunk + t, first + min((u + 1) * chunk, n), kRowThreads, bound, list, WideTop::list_size(k), &sh.n[s]);
+                collect(row, first + u * chunk + (t / 32 + u) % kWarps * 32 + t % 32, first + min((u + 1) * chunk, n), kRowThreads, bound, list,
+                        WideTop::list_size(k), &sh.n[s]);
         }
     __syncwarp();
     if (m > kPlaces || sh.n[s] > WideTop::list_size(k)) collect_exact<32>(row, first, n, k, sh, s);
@@ -1094,10 +1130,10 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
     const int cta_n = plan.cta_n, slot_bytes = plan.chunk * 16;
     const uint32_t rank = cluster_rank();
     const int groups = gridDim.x / cta_n, group = blockIdx.x / cta_n;
-    const int rows = (a.n - group + groups - 1) / groups;  // row q of the cluster is group + q groups
     const int first = rank * plan.per_cta;
     const uint32_t full = smem_addr(sm.full), empty = smem_addr(sm.empty);
     const uint32_t info_full = smem_addr(sm.info_full), info_empty = smem_addr(sm.info_empty);
+    const uint32_t claim_full = smem_addr(sm.claim_full);
     const uint32_t parts_full = smem_addr(sm.parts_full), coef_full = smem_addr(sm.coef_full);
     auto slot_of = [](int q) { return q % kSlots; };
     auto parity_of = [](int q) { return (uint32_t)(q / kSlots) & 1; };
@@ -1122,6 +1158,8 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
                 mbar_init(smem_addr(&sh.best_full[k]), 1);
             }
         }
+        for (int k = 0; k < kClaims; ++k) mbar_init(claim_full + 8 * k, 1);
+        sm.last = INT_MAX;
         sm.dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -1141,10 +1179,29 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
         int32_t tok = 0;
         float x_tok = NAN, w = 1.f, adv = 0.f, old = 0.f;
         T edge = from_f32<T>(kNegInf);
+        // The cluster's q-th row, -1: there is none. Without claims the clusters take the rows in turn; with them a
+        // cluster begins with its own and takes over another's when it has begun its last.
+        auto row_of = [&](int q) -> int64_t {
+            if (!plan.claims) {
+                const int64_t i = group + (int64_t)q * groups;
+                return i < a.n ? i : -1;
+            }
+            if (q == 0) return group;
+            const int claim = q - 1;  // (the first row is the cluster's own)
+            mbar_wait_idle(claim_full + 8 * (claim % kClaims), claim / kClaims & 1, &sm.dead);
+            if (*(volatile int*)&sm.dead || q >= *(volatile int*)&sm.last) return -1;
+            const int cta = claimed_cta(smem_addr(&sm.claim[claim % kClaims]));
+            return cta < 0 || cta / cta_n >= a.n ? -1 : cta / cta_n;
+        };
+        auto claim_next = [&](int q) {  // the row after q; every CTA's helper
+            if (!plan.claims || lane != 0) return;
+            const uint32_t bar = claim_full + 8 * (q % kClaims);  // (claim q is row q + 1)
+            mbar_expect(bar, 16);
+            if (rank == 0) claim_cluster(smem_addr(&sm.claim[q % kClaims]), bar, cta_n == 1);
+        };
         // (a gradient in place comes later: it waits for this row's copy, which waits for this)
-        auto look = [&](int q) {
-            const int64_t i = group + (int64_t)q * groups;
-            if (OP == OP_DISTILL || q >= rows) return;
+        auto look = [&](int64_t i) {
+            if (OP == OP_DISTILL || i < 0) return;
             const Row<T> row(a, i);
             tok = a.tokens ? a.tokens[i] : 0;
             if (OP == OP_POLICY && lane == 0) {
@@ -1158,9 +1215,27 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
                 if (lane == 0 && a.tokens && tok < row.vocab) x_tok = to_f32(row.x[tok]);
             }
         };
-        look(s);
-        for (int q = s; q < rows; q += kSlots) {
-            const int64_t i = group + (int64_t)q * groups;
+        int64_t next = plan.claims ? -1 : row_of(s);
+        look(next);
+        for (int q = s;; q += kSlots) {
+            if (plan.claims) {
+                next = row_of(q);
+                look(next);
+            }
+            const int64_t i = next;
+            if (i < 0) {
+                mbar_wait_idle(info_empty + 8 * s, parity_of(q) ^ 1, &sm.dead);
+                if (lane == 0) {
+                    info.end = 1;
+                    info.live = 0;
+                    mbar_arrive(info_full + 8 * s);
+                    if (plan.claims && q <= *(volatile int*)&sm.last) {  // the helpers that wait for the rows after
+                        *(volatile int*)&sm.last = q;
+                        for (int d = 0; d < kSlots - 1; ++d) mbar_arrive(claim_full + 8 * ((q + d) % kClaims));
+                    }
+                }
+                break;
+            }
             const Row<T> row(a, i);
             if (OP == OP_DISTILL) edge = edge_element(row, first, plan.per_cta);
             mbar_wait_idle(info_empty + 8 * s, parity_of(q) ^ 1, &sm.dead);
@@ -1181,6 +1256,7 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
             };
             if (lane == 0) {
                 info.row = row;
+                info.end = 0;
                 info.live = OP == OP_DISTILL ? teacher.live : tok >= 0;
             }
             if (TOP && lane == 0) sh.n[s] = 0;
@@ -1189,11 +1265,16 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
             if (in_place) own_values();
             __syncwarp();
             if (lane == 0) mbar_arrive(info_full + 8 * s);
+            if (!GRAD) claim_next(q);
             if (!in_place) own_values();
             __syncwarp();
-            look(q + kSlots);
+            if (!plan.claims) {
+                next = row_of(q + kSlots);
+                look(next);
+            }
             // ---- the row's results, from all parts in the same order
             mbar_wait_idle(parts_full + 8 * s, parity_of(q), &sm.dead);
+            if (GRAD) claim_next(q);  // (half of the row's time is left)
             Stats all;
             float bound = kNegInf;
             bool low = false;
@@ -1251,9 +1332,10 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
         // ---- the copies
         if (lane == 0) {
             int slot = 0, phase = 0;
-            for (int q = 0; q < rows; ++q) {
+            for (int q = 0;; ++q) {
                 const int s = slot_of(q);
                 mbar_wait(info_full + 8 * s, parity_of(q), &sm.dead);
+                if (sm.info[s].end || *(volatile int*)&sm.dead) break;
                 const bool live = sm.info[s].live;
                 const Row<T> row = sm.info[s].row;
                 const uint4 head = sm.info[s].edge[0], tail = sm.info[s].edge[1];
@@ -1297,7 +1379,6 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
 
         auto statistics = [&](int q) {
             const int s = slot_of(q);
-            mbar_wait(info_full + 8 * s, parity_of(q), &sm.dead);
             Running run;
             float bound = kNegInf;
             if (sm.info[s].live) {
@@ -1380,14 +1461,16 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
                 }
                 own_terms<T, OP, ENT>(row, info, f, c, list_at(s), [&](int id) {
                     const int v = (id + row.lead) / E - first;
-                    return v >= 0 && v < slice.n && v % plan.chunk / 32 % kWarps == warp;
+                    return v >= 0 && v < slice.n && (unsigned)(v % plan.chunk / 32 - v / plan.chunk) % kWarps == (unsigned)warp;
                 });
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(info_empty + 8 * s);
         };
 
-        for (int q = 0; q < rows; ++q) {
+        for (int q = 0;; ++q) {
+            mbar_wait(info_full + 8 * slot_of(q), parity_of(q), &sm.dead);
+            if (sm.info[slot_of(q)].end || *(volatile int*)&sm.dead) break;
             statistics(q);
             if constexpr (GRAD) rest(q);
         }
@@ -1404,13 +1487,11 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
 // 1 us of a CTA: helpers, barriers, exchange) would be most of a short row's time.
 constexpr int kNarrowWarps = 4;
 constexpr int kNarrowBytes = 32768;
-typedef TopShared<kNarrowWarps * 32, 1> NarrowTop;
 
 template <typename T, int OP, bool GRAD, bool ENT, bool TOP, int TEAM>
 __global__ void __launch_bounds__(kNarrowWarps * 32) narrow_kernel(const __grid_constant__ RowArgs a) {
     extern __shared__ __align__(16) uint8_t space[];
     constexpr int kRows = kNarrowWarps / TEAM, kTeam = TEAM * 32;
-    static_assert(!TOP || TEAM == kNarrowWarps);
     __shared__ RowInfo<T> infos[kRows];
     __shared__ float4 parts[kNarrowWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, team = warp / TEAM, t = threadIdx.x - team * kTeam;
@@ -1429,7 +1510,8 @@ __global__ void __launch_bounds__(kNarrowWarps * 32) narrow_kernel(const __grid_
     const int list_bytes = kSeenWords * 4 + a.k * TeacherList::kBytes;
     uint32_t* seen = (uint32_t*)(space + team * list_bytes);
     const TeacherList list(space + team * list_bytes + kSeenWords * 4, a.k);
-    NarrowTop& sh = *(NarrowTop*)space;
+    typedef TopShared<kTeam, 1> NarrowTop;
+    NarrowTop& sh = *(NarrowTop*)(space + team * (TOP ? NarrowTop::bytes(a.k, 1) : 0));
     if constexpr (OP == OP_DISTILL) {
         if (t < 32) {
             for (int k = lane; k < kSeenWords; k += 32) seen[k] = 0;
@@ -1511,7 +1593,11 @@ __global__ void __launch_bounds__(kNarrowWarps * 32) narrow_kernel(const __grid_
     if constexpr (TOP) {
         Key* keys = sh.list(0, a.k);
         if (live) {
-            const float bound = kth_of_maxima<kTeam>(sh.most[0], a.k, kNegInf);
+            float bound = kNegInf;
+            if constexpr (TEAM > 1)
+                bound = kth_of_maxima<kTeam>(sh.most[0], a.k, kNegInf);
+            else if (a.k <= 32)
+                bound = warp_kth(run.m, a.k - 1);
             const int size = NarrowTop::list_size(a.k);
             if (run.m >= bound) collect(row, t, row.n_vec, kTeam, bound, keys, size, &sh.n[0]);
             sync();
@@ -1520,7 +1606,7 @@ __global__ void __launch_bounds__(kNarrowWarps * 32) narrow_kernel(const __grid_
                 collect_exact<kTeam>(row, 0, row.n_vec, a.k, sh, 0);
             }
         }
-        if (warp == 0) alternatives(a, i, sh, 0, 0, 0, 1, res, nullptr);
+        if (t < 32) alternatives(a, i, sh, 0, 0, 0, 1, res, nullptr);
     }
 }
 
@@ -1528,24 +1614,27 @@ __global__ void __launch_bounds__(kNarrowWarps * 32) narrow_kernel(const __grid_
 constexpr int kBackThreads = 256;
 constexpr int kBackVecs = 4;  // a thread's, all loaded before the first is used
 
+// A warp takes 128 neighbouring vectors of a row, whatever the row's length.
 template <typename T, bool ENT>
-__global__ void __launch_bounds__(kBackThreads) backward_kernel(const RowArgs a, int ctas_per_row) {
+__global__ void __launch_bounds__(kBackThreads) backward_kernel(const __grid_constant__ RowArgs a, uint32_t units, uint32_t units_per_row) {
     constexpr int E = Vec<T>::E;
-    const int64_t i = blockIdx.x / ctas_per_row;
-    const int first = (int)(blockIdx.x % ctas_per_row) * kBackThreads * kBackVecs + threadIdx.x;
-    const Row<T> row(a, i);
     after_predecessor();
+    const uint32_t unit = (blockIdx.x * kBackThreads + threadIdx.x) / 32;
+    if (unit >= units) return;
+    const int64_t i = unit / units_per_row;
+    const int first = (int)(unit - (uint32_t)i * units_per_row) * 32 * kBackVecs + (threadIdx.x & 31);
+    const Row<T> row(a, i);
     const int32_t tok = a.tokens ? a.tokens[i] : 0;
     if (tok < 0) {
         const uint4 zero = make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int u = 0; u < kBackVecs; ++u) row.store(first + u * kBackThreads, zero, first + u * kBackThreads < row.n_vec);
+        for (int u = 0; u < kBackVecs; ++u) row.store(first + 32 * u, zero, first + 32 * u < row.n_vec);
         return;
     }
     uint4 r[kBackVecs];
 #pragma unroll
     for (int u = 0; u < kBackVecs; ++u)
-        r[u] = first + u * kBackThreads < row.n_vec ? row.load(first + u * kBackThreads) : make_uint4(0, 0, 0, 0);
+        r[u] = first + 32 * u < row.n_vec ? row.load(first + 32 * u) : make_uint4(0, 0, 0, 0);
     const float inv_t = 1.f / a.temperature;
     float lse = a.lse_in[i], k0 = 0.f, k1 = 0.f, k2 = 0.f;  // gradient p (k0 + k1 ln p) + [j = token] k2
     if (a.dlogp) {
@@ -1564,7 +1653,7 @@ __global__ void __launch_bounds__(kBackThreads) backward_kernel(const RowArgs a,
     const int tok_vec = a.dlogp && tok < row.vocab ? (tok + row.lead) / E : -1;
 #pragma unroll
     for (int u = 0; u < kBackVecs; ++u) {
-        const int v = first + u * kBackThreads;
+        const int v = first + 32 * u;
         float x[E];
         Vec<T>::unpack(r[u], x);
 #pragma unroll
@@ -1588,10 +1677,10 @@ __global__ void __launch_bounds__(kBackThreads) backward_kernel(const RowArgs a,
 
 // ---------------------------------------------------------------- launches --
 template <typename... P, typename... A>
-cudaError_t launch_kernel(void (*kernel)(P...), int64_t ctas, int cluster, int threads, int smem, cudaStream_t s, A&&... args) {
+cudaError_t launch_kernel(void (*kernel)(P...), int64_t ctas, int cluster, bool early, int threads, int smem, cudaStream_t s, A&&... args) {
     cudaLaunchAttribute attr[2] = {};
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[0].val.programmaticStreamSerializationAllowed = early;
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = cluster;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
@@ -1634,7 +1723,7 @@ struct Launch {
 // lists of alternatives leave room for one CTA an SM only. False: too large.
 bool make_launch(const Shape& h, Launch& out) {
     constexpr int kSmBytes = 233472, kReserved = 1024;
-    constexpr int64_t kRowsInL2 = 48ll << 20;
+    constexpr int64_t kRowsInL2 = 48ll << 20, kClaimBytes = 64 << 10;
     constexpr int kChunkVecs = 4 * kRowThreads, kAtLeast = 3 * kChunkVecs * 16;  // of a ring
     // clusters of 1, 2, 4 and 8 CTAs that the GPU holds at once, one or two CTAs an SM
     static const int kClusters[2][4] = {{152, 76, 36, 15}, {304, 152, 74, 36}};
@@ -1662,6 +1751,11 @@ bool make_launch(const Shape& h, Launch& out) {
     const bool two = half - behind >= kAtLeast;
     plan.chunks = std::min(kMaxChunks, ((two ? half : whole) - behind) / (plan.chunk * 16));
     out.clusters = std::min(h.n, kClusters[two][size]);
+    // Claims even out what padding and the SMs' own pace leave. A claim takes about 1 us, a few at the end are not ahead
+    // of anything: of rows in few rounds, or short ones, each cluster has its own (1000x50001 fp16 in 3.3 rounds 26 us,
+    // with claims 30; 4096x131072 bf16 in 27 of 10% padding 347, 320).
+    plan.claims = h.n >= 6 * out.clusters && (int64_t)plan.per_cta * 16 >= kClaimBytes;
+    if (plan.claims) out.clusters = h.n;
     out.smem = plan.chunks * plan.chunk * 16 + behind;
     return plan.chunks >= 2 && out.smem <= whole;
 }
@@ -1669,9 +1763,9 @@ bool make_launch(const Shape& h, Launch& out) {
 template <typename T, int OP, bool GRAD, bool ENT, bool TOP, int TEAM>
 cudaError_t launch_narrow(const RowArgs& a, cudaStream_t s) {
     constexpr int kRows = kNarrowWarps / TEAM;
-    const int bytes = TOP ? NarrowTop::bytes(a.k, 1) : OP == OP_DISTILL ? kRows * (kSeenWords * 4 + a.k * TeacherList::kBytes) : 0;
+    const int bytes = TOP ? kRows * TopShared<TEAM * 32, 1>::bytes(a.k, 1) : OP == OP_DISTILL ? kRows * (kSeenWords * 4 + a.k * TeacherList::kBytes) : 0;
     static_assert(kNarrowWarps * (kSeenWords * 4 + TP_MAX_TEACHER_LOGITS * TeacherList::kBytes) + 1024 <= 48 * 1024);
-    return launch_kernel(narrow_kernel<T, OP, GRAD, ENT, TOP, TEAM>, (a.n + (int64_t)kRows - 1) / kRows, 0, kNarrowWarps * 32, bytes, s, a);
+    return launch_kernel(narrow_kernel<T, OP, GRAD, ENT, TOP, TEAM>, (a.n + (int64_t)kRows - 1) / kRows, 0, true, kNarrowWarps * 32, bytes, s, a);
 }
 
 template <typename T, int OP, bool GRAD, bool ENT, bool TOP = false>
@@ -1679,8 +1773,7 @@ cudaError_t launch_rows(const RowArgs& a, cudaStream_t s) {
     constexpr int E = Vec<T>::E;
     if ((int64_t)a.vocab * (int)sizeof(T) <= kNarrowBytes) {
         // one warp a row where it has at most four vectors for a lane and there are enough rows to fill the GPU
-        if constexpr (!TOP)
-            if (a.vocab * (int)sizeof(T) <= 2048 && a.n >= 2048) return launch_narrow<T, OP, GRAD, ENT, false, 1>(a, s);
+        if (a.vocab * (int)sizeof(T) <= 2048 && a.n >= 2048 && (!TOP || a.k <= 32)) return launch_narrow<T, OP, GRAD, ENT, TOP, 1>(a, s);
         return launch_narrow<T, OP, GRAD, ENT, TOP, kNarrowWarps>(a, s);
     }
     // (rows that all begin in a line of their own have one vector less than rows at any place)
@@ -1700,14 +1793,16 @@ cudaError_t launch_rows(const RowArgs& a, cudaStream_t s) {
         if (e != cudaSuccess) return e;
         allowed.fetch_or(bit, std::memory_order_relaxed);
     }
-    return launch_kernel(kernel, (int64_t)l.clusters * l.plan.cta_n, l.plan.cta_n, kThreads, l.smem, s, a, l.plan);
+    return launch_kernel(kernel, (int64_t)l.clusters * l.plan.cta_n, l.plan.cta_n, !l.plan.claims, kThreads, l.smem, s, a, l.plan);
 }
 
 template <typename T, bool ENT>
 cudaError_t launch_back(const RowArgs& a, cudaStream_t s) {
-    constexpr int E = Vec<T>::E, per_cta = kBackThreads * kBackVecs;
-    const int ctas = ((a.vocab + 2 * E - 2) / E + per_cta - 1) / per_cta;
-    return launch_kernel(backward_kernel<T, ENT>, (int64_t)a.n * ctas, 0, kBackThreads, 0, s, a, ctas);
+    constexpr int E = Vec<T>::E, kWarp = 32 * kBackVecs;
+    const int64_t per_row = ((a.vocab + 2 * E - 2) / E + kWarp - 1) / kWarp, units = a.n * per_row;
+    if (units > INT_MAX) return cudaErrorInvalidConfiguration;  // (4 TB of logits)
+    return launch_kernel(backward_kernel<T, ENT>, (units * 32 + kBackThreads - 1) / kBackThreads, 0, true, kBackThreads, 0, s, a,
+                         (uint32_t)units, (uint32_t)per_row);
 }
 
 }  // namespace
