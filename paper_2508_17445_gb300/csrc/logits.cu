@@ -219,7 +219,6 @@ __device__ __forceinline__ void threads_sync() {
     else
         asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
 }
-__device__ __forceinline__ void row_threads_sync() { threads_sync<kRowThreads>(); }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
@@ -717,7 +716,7 @@ struct TopShared {
     // 0 where none is left
 
     static __host__ __device__ __forceinline__ int list_size(int k) { return 4 * k + 64; }
-    static __host__ __forceinline__ int bytes(int k, int cta_n) {
+    static __host__ __device__ __forceinline__ int bytes(int k, int cta_n) {
         return (int)sizeof(TopShared) + SLOTS * 8 * (list_size(k) + (cta_n > 1 ? cta_n * k : 0));
     }
     __device__ __forceinline__ Key* list(int s, int k) { return (Key*)(this + 1) + s * list_size(k); }
@@ -946,15 +945,50 @@ __device__ __forceinline__ void collect_parts(const Row<T>& row, int first, int 
             m += __popc(hits);
         }
     __syncwarp();
-    if (m <= kPlaces)
-        for (int p = lane; p < m; p += 32) {  // a lane's loads are in flight with the others'
-            const int t = sh.place[s][p] % kRowThreads, u0 = sh.place[s][p] / kRowThreads * per_part;
-            for (int u = u0; u < min(u0 + per_part, chunks); ++u)
-                collect(row, first + u * chunk + (t / 32 + u) % kWarps * 32 + t % 32, first + min((u + 1) * chunk, n), kRowThreads, bound, list,
-                        WideTop::list_size(k), &sh.n[s]);
+    // the vectors there that hold such logits (kHits of them at most), then their logits
+    constexpr int kHits = 256;
+    int* hit_vec = sh.hist[s];
+    int hits = 0;
+    for (int p0 = 0; p0 < m && m <= kPlaces; p0 += 32) {
+        const int at = p0 + lane < m ? sh.place[s][p0 + lane] : 0, t = at % kRowThreads;
+        for (int du = 0; du < per_part; ++du) {
+            const int u = at / kRowThreads * per_part + du, g = (t / 32 + u) % kWarps * 32 + t % 32;
+            const int v0 = first + u * chunk + g, end = p0 + lane < m && u < chunks ? first + min((u + 1) * chunk, n) : 0;
+            for (int j = 0; j < chunk; j += 4 * kRowThreads) {
+                uint4 r[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int v = v0 + j + k * kRowThreads;
+                    r[k] = make_uint4(Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone);
+                    if (v < end) r[k] = row.load_kept(v);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float most = Vec<T>::template max_of<1>(r + k);
+                    const bool hit = most >= bound && most > kNegInf;
+                    const uint32_t who = __ballot_sync(0xffffffffu, hit);
+                    const int place = hits + __popc(who & ((1u << lane) - 1));
+                    if (hit && place < kHits) hit_vec[place] = v0 + j + k * kRowThreads;
+                    hits += __popc(who);
+                }
+            }
+        }
+    }
+    __syncwarp();
+    if (hits <= kHits)
+        for (int h = lane; h < hits; h += 32) {
+            const int v = hit_vec[h];
+            float x[Vec<T>::E];
+            Vec<T>::unpack(row.load_kept(v), x);
+#pragma unroll
+            for (int e = 0; e < Vec<T>::E; ++e)
+                if (x[e] >= bound && x[e] > kNegInf) {
+                    const int place = atomicAdd(&sh.n[s], 1);
+                    if (place < WideTop::list_size(k)) list[place] = make_key(x[e], v * Vec<T>::E + e - row.lead);
+                }
         }
     __syncwarp();
-    if (m > kPlaces || sh.n[s] > WideTop::list_size(k)) collect_exact<32>(row, first, n, k, sh, s);
+    if (m > kPlaces || hits > kHits || sh.n[s] > WideTop::list_size(k)) collect_exact<32>(row, first, n, k, sh, s);
 }
 
 // One helper warp: the row's alternatives from the CTAs' lists.
@@ -1152,7 +1186,7 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
         for (int k = 0; k < kSlots; ++k) {
             mbar_init(info_full + 8 * k, 1);
             mbar_init(info_empty + 8 * k, kWarps + 1);
-            mbar_init(parts_full + 8 * k, 1);
+            mbar_init(parts_full + 8 * k, TOP ? kWarps : 1);  // (TOP: what every warp left for the helper)
             mbar_init(coef_full + 8 * k, 1);
             if constexpr (TOP) {
                 mbar_init(smem_addr(&sh.best_full[k]), 1);
@@ -1387,6 +1421,9 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
                 const int chunks = slice.chunks();
                 const int per_part = (chunks + kCells - 1) / kCells;
                 float part = kNegInf;
+                __nv_bfloat16* to = nullptr;  // the part's place
+                int left = per_part;          // the part's chunks to come
+                if constexpr (TOP) to = &sh.part[s][0][tid];
                 for (int k = 0; k < chunks; ++k) {
                     const uint8_t* data = chunk_here();
                     slice.template each<4>(data, k, [&](auto count, const uint4* r, int, bool) {
@@ -1394,9 +1431,11 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
                         if (TOP) part = fmaxf(part, m2);
                     });
                     chunk_done();
-                    if (TOP && ((k + 1) % per_part == 0 || k + 1 == chunks)) {
-                        sh.part[s][k / per_part][tid] = __float2bfloat16_ru(part);
+                    if (TOP && (--left == 0 || k + 1 == chunks)) {
+                        *to = __float2bfloat16_ru(part);
                         part = kNegInf;
+                        to += kRowThreads;
+                        left = per_part;
                     }
                 }
             }
@@ -1409,8 +1448,11 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
             const bool low = GRAD && ENT && __any_sync(0xffffffffu, run.low);
             // (a gradient waits for its row's, see there: no CTA of the cluster is more than three rows ahead of a helper)
             if (!GRAD && q >= 2) mbar_wait(coef_full + 8 * slot_of(q - 2), parity_of(q - 2), &sm.dead);
-            if (TOP) row_threads_sync();  // (the helper reads what all threads left)
-            if (tid == 0) mbar_expect(parts_full + 8 * s, cta_n * kWarps * 16);
+            if (TOP) __syncwarp();
+            if (tid == 0)
+                mbar_expect(parts_full + 8 * s, cta_n * kWarps * 16);
+            else if (TOP && lane == 0)
+                mbar_arrive(parts_full + 8 * s);
             if (lane < cta_n)
                 send(map_to(smem_addr(&sm.parts[s][rank][warp]), lane), map_to(parts_full + 8 * s, lane), st.m, st.s, st.t,
                      TOP ? bound : low ? 1.f : 0.f);
@@ -1614,27 +1656,30 @@ __global__ void __launch_bounds__(kNarrowWarps * 32) narrow_kernel(const __grid_
 constexpr int kBackThreads = 256;
 constexpr int kBackVecs = 4;  // a thread's, all loaded before the first is used
 
-// A warp takes 128 neighbouring vectors of a row, whatever the row's length.
-template <typename T, bool ENT>
+// A CTA takes 1024 neighbouring vectors of a row, each warp 32 of every 256; of rows
+// shorter than that each warp 128 of a row (WARPS; 8192x1000 25 us by CTAs, 8 by
+// warps; 4096x131072 303 by CTAs, 313 by warps).
+template <typename T, bool ENT, bool WARPS>
 __global__ void __launch_bounds__(kBackThreads) backward_kernel(const __grid_constant__ RowArgs a, uint32_t units, uint32_t units_per_row) {
     constexpr int E = Vec<T>::E;
     after_predecessor();
-    const uint32_t unit = (blockIdx.x * kBackThreads + threadIdx.x) / 32;
+    constexpr int kUnit = WARPS ? 32 : kBackThreads;  // threads, and vectors between a thread's
+    const uint32_t unit = WARPS ? (blockIdx.x * kBackThreads + threadIdx.x) / 32 : blockIdx.x;
     if (unit >= units) return;
     const int64_t i = unit / units_per_row;
-    const int first = (int)(unit - (uint32_t)i * units_per_row) * 32 * kBackVecs + (threadIdx.x & 31);
+    const int first = (int)(unit - (uint32_t)i * units_per_row) * kUnit * kBackVecs + threadIdx.x % kUnit;
     const Row<T> row(a, i);
     const int32_t tok = a.tokens ? a.tokens[i] : 0;
     if (tok < 0) {
         const uint4 zero = make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int u = 0; u < kBackVecs; ++u) row.store(first + 32 * u, zero, first + 32 * u < row.n_vec);
+        for (int u = 0; u < kBackVecs; ++u) row.store(first + kUnit * u, zero, first + kUnit * u < row.n_vec);
         return;
     }
     uint4 r[kBackVecs];
 #pragma unroll
     for (int u = 0; u < kBackVecs; ++u)
-        r[u] = first + 32 * u < row.n_vec ? row.load(first + 32 * u) : make_uint4(0, 0, 0, 0);
+        r[u] = first + kUnit * u < row.n_vec ? row.load(first + kUnit * u) : make_uint4(0, 0, 0, 0);
     const float inv_t = 1.f / a.temperature;
     float lse = a.lse_in[i], k0 = 0.f, k1 = 0.f, k2 = 0.f;  // gradient p (k0 + k1 ln p) + [j = token] k2
     if (a.dlogp) {
@@ -1653,7 +1698,7 @@ __global__ void __launch_bounds__(kBackThreads) backward_kernel(const __grid_con
     const int tok_vec = a.dlogp && tok < row.vocab ? (tok + row.lead) / E : -1;
 #pragma unroll
     for (int u = 0; u < kBackVecs; ++u) {
-        const int v = first + 32 * u;
+        const int v = first + kUnit * u;
         float x[E];
         Vec<T>::unpack(r[u], x);
 #pragma unroll
@@ -1798,11 +1843,15 @@ cudaError_t launch_rows(const RowArgs& a, cudaStream_t s) {
 
 template <typename T, bool ENT>
 cudaError_t launch_back(const RowArgs& a, cudaStream_t s) {
-    constexpr int E = Vec<T>::E, kWarp = 32 * kBackVecs;
-    const int64_t per_row = ((a.vocab + 2 * E - 2) / E + kWarp - 1) / kWarp, units = a.n * per_row;
+    constexpr int E = Vec<T>::E;
+    const int n_vec = (a.vocab + 2 * E - 2) / E;
+    const bool warps = n_vec < kBackThreads * kBackVecs;
+    const int unit = (warps ? 32 : kBackThreads) * kBackVecs;
+    const int64_t per_row = (n_vec + unit - 1) / unit, units = a.n * per_row;
     if (units > INT_MAX) return cudaErrorInvalidConfiguration;  // (4 TB of logits)
-    return launch_kernel(backward_kernel<T, ENT>, (units * 32 + kBackThreads - 1) / kBackThreads, 0, true, kBackThreads, 0, s, a,
-                         (uint32_t)units, (uint32_t)per_row);
+    return launch_kernel(warps ? backward_kernel<T, ENT, true> : backward_kernel<T, ENT, false>,
+                         warps ? (units * 32 + kBackThreads - 1) / kBackThreads : units, 0, true, kBackThreads, 0, s, a, (uint32_t)units,
+                         (uint32_t)per_row);
 }
 
 }  // namespace
