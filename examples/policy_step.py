@@ -1,0 +1,167 @@
+"""A policy update over a sampled tree, and distillation from a teacher.
+
+The calls of the library in the order in which a TreePO training program makes
+them, around a toy policy (an embedding, one attention layer over the segment
+tree, an output matrix; PyTorch matmuls stand for the caller's model):
+
+  sampling   tp_append_tokens + tp_decode, tp_token_logprobs for the top
+             alternatives of every live path, one of which is taken
+  branching  the segments' mean log probabilities split the budget
+             (tp_branch_assign), paths fork
+  rewards    tp_tree_advantage over the node table
+  update     tp_policy_loss: loss and gradient of every sampled token's logits
+  distill    a teacher's top logits (tp_token_logprobs) to tp_distill_loss
+
+Only the output matrix learns. Run:  python examples/policy_step.py
+"""
+from __future__ import annotations
+
+import os
+import sys
+
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+import paper_2508_17445_gb300 as tp  # noqa: E402
+
+DEV = "cuda:0"
+
+
+class Policy:
+    """logits = attention(tree, q(e_token)) W for the last token of every path."""
+
+    def __init__(self, vocab: int, heads=(8, 2, 64), seed: int = 0):
+        g = torch.Generator(device=DEV).manual_seed(seed)
+        self.vocab, (self.hq, self.hkv, self.hd) = vocab, heads
+        rnd = lambda *s: torch.randn(s, generator=g, device=DEV)  # noqa: E731
+        self.embed = rnd(vocab, 3, self.hq, self.hd).bfloat16()  # q, and in its first kv heads k, v
+        self.out = 0.05 * rnd(self.hq * self.hd, vocab)          # fp32 master copy
+
+    def qkv(self, tokens):
+        e = self.embed[tokens.long()]
+        return e[:, 0].contiguous(), e[:, 1, : self.hkv].contiguous(), e[:, 2, : self.hkv].contiguous()
+
+    def logits(self, hidden):
+        return hidden @ self.out.bfloat16()
+
+
+def sample_tree(policy: Policy, prompts: int, width: int, depth: int, segment: int, temperature: float, top: int, gen):
+    """Trees of `prompts` prompts grown to `width` paths; returns what the update takes."""
+    forest = tp.Forest(policy.hq, policy.hkv, policy.hd, pool_blocks=prompts * width * (depth * (segment // 32 + 2) + 2), device=DEV)
+    parent, live, last = [], [], []  # node table; live paths' nodes and last tokens
+    node_of = {}
+
+    def node(forest_node, up):
+        node_of[forest_node] = len(parent)
+        parent.append(up)
+
+    for _ in range(prompts):
+        root = forest.add_root()
+        node(root, -1)
+        tokens = torch.randint(0, policy.vocab, (40,), generator=gen, device=DEV)
+        _, k, v = policy.qkv(tokens)
+        forest.append(root, k, v)
+        live.append(root)
+        last.append(tokens[-1:])
+    last = torch.cat(last).int()
+    steps = []  # (hidden, tokens, log probabilities, node table index of each row)
+    for d in range(depth):
+        # every path goes on in a new segment; paths whose last one was likelier branch more often
+        n = len(live)
+        budget = max(n, min(prompts * width, 2 * n))
+        if d == 0:
+            kids = tp.tp_branch_assign(None, n, budget, tp.TP_BRANCH_EVEN)
+        else:
+            kids = tp.tp_branch_assign(mean_logp.tolist(), n, budget, tp.TP_BRANCH_LOGP_HIGH, 2.0)  # noqa: F821
+        grown, rows = [], []
+        for i, (leaf, k) in enumerate(zip(live, kids)):
+            for child in forest.fork(leaf, k):
+                node(child, node_of[leaf])
+                grown.append(child)
+                rows.append(i)
+        live, last = grown, last[torch.tensor(rows, device=DEV)]
+        n = len(live)
+        at = torch.tensor([node_of[x] for x in live], device=DEV)
+        total = torch.zeros(n, device=DEV)
+        ids, logp = torch.empty((n, top), dtype=torch.int32, device=DEV), torch.empty((n, top), device=DEV)
+        for _ in range(segment):
+            q, k, v = policy.qkv(last)
+            forest.append_tokens(live, k, v)
+            hidden = forest.decode(live, q)[0].view(n, -1)
+            tp.tp_token_logprobs(policy.logits(hidden), top_ids=ids, top_logp=logp, temperature=temperature)
+            pick = torch.multinomial(logp.exp(), 1, generator=gen)
+            last = ids.gather(1, pick)[:, 0].contiguous()
+            chosen = logp.gather(1, pick)[:, 0]
+            steps.append((hidden, last, chosen, at))
+            total += chosen
+        mean_logp = (total / segment).cpu()
+    leaves = torch.tensor([node_of[x] for x in live], dtype=torch.int32, device=DEV)
+    forest.close()
+    hidden, tokens, old, at = (torch.cat(x) for x in zip(*steps))
+    return dict(hidden=hidden, tokens=tokens, old_logp=old, node=at, parent=torch.tensor(parent, dtype=torch.int32, device=DEV),
+                leaves=leaves)
+
+
+def advantages(tree, reward):
+    """The mean advantage of the trajectories through each sampled token's segment."""
+    n = len(tree["leaves"])
+    adv = torch.empty(n, device=DEV)
+    tp.tp_tree_advantage(tree["parent"], tree["leaves"], reward, adv)
+    nodes = len(tree["parent"])
+    total, count = torch.zeros(nodes, device=DEV), torch.zeros(nodes, device=DEV)
+    x, up = tree["leaves"].long(), tree["parent"].long()
+    while bool((x >= 0).any()):
+        some = x >= 0
+        total.index_add_(0, x[some], adv[some])
+        count.index_add_(0, x[some], torch.ones_like(adv[some]))
+        x = torch.where(some, up[x.clamp(min=0)], x)
+    return (total / count.clamp(min=1))[tree["node"]].contiguous()
+
+
+def update(policy: Policy, tree, reward, temperature: float, rate: float):
+    """One gradient step on the output matrix; returns the loss and the mean entropy."""
+    n = len(tree["tokens"])
+    logits = policy.logits(tree["hidden"])
+    loss, entropy, grad = torch.empty(n, device=DEV), torch.empty(n, device=DEV), torch.empty_like(logits)
+    # (the sampled alternatives' log probabilities are those of the whole distribution)
+    tp.tp_policy_loss(logits, tree["tokens"], advantages(tree, reward), loss, grad, tree["old_logp"],
+                      torch.full((n,), 1.0 / n, device=DEV), entropy=entropy, clip_low=0.2, clip_high=0.28, entropy_coef=1e-3,
+                      temperature=temperature)
+    policy.out -= rate * (tree["hidden"].t() @ grad).float()
+    return float(loss.sum()), float(entropy.mean())
+
+
+def distill(policy: Policy, teacher: Policy, hidden, top: int, rate: float):
+    """One step towards the teacher's top logits; returns the loss."""
+    n = len(hidden)
+    ids, logp = torch.empty((n, top), dtype=torch.int32, device=DEV), torch.empty((n, top), device=DEV)
+    tp.tp_token_logprobs(teacher.logits(hidden), top_ids=ids, top_logp=logp)
+    logits = policy.logits(hidden)
+    loss = torch.empty(n, device=DEV)
+    tp.tp_distill_loss(logits, ids, logp, loss, logits, torch.full((n,), 1.0 / n, device=DEV))  # the gradient in place
+    policy.out -= rate * (hidden.t() @ logits).float()
+    return float(loss.sum())
+
+
+def main(steps: int = 6, vocab: int = 2000, prompts: int = 4, width: int = 8, depth: int = 3, segment: int = 12):
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    policy, student, teacher = Policy(vocab, seed=0), Policy(vocab, seed=0), Policy(vocab, seed=0)
+    teacher.out = Policy(vocab, seed=5).out * 2
+    rewards = []
+    for i in range(steps):
+        tree = sample_tree(policy, prompts, width, depth, segment, 1.0, 32, gen)
+        # rewarded: trajectories whose last segment holds many even tokens
+        even = (tree["tokens"] % 2 == 0).float()
+        per_node = torch.zeros(len(tree["parent"]), device=DEV).index_add_(0, tree["node"], even) / segment
+        reward = per_node[tree["leaves"].long()].contiguous()
+        loss, entropy = update(policy, tree, reward, 1.0, 60.0)
+        rewards.append(float(even.mean()))
+        print(f"step {i}: {len(tree['leaves'])} trajectories, {len(tree['tokens'])} tokens, even {rewards[-1]:.3f}, "
+              f"loss {loss:+.4f}, entropy {entropy:.3f}")
+    kl = [distill(student, teacher, tree["hidden"], 32, 0.3) for _ in range(5)]
+    print("distillation:", " ".join(f"{x:.4f}" for x in kl))
+    return rewards, kl
+
+
+if __name__ == "__main__":
+    main()

@@ -510,3 +510,98 @@ def test_binding_refuses():
         tp.tp_token_logprobs(x[:1].expand(4, 100), tok, one)
     e = torch.empty(0, device=DEV)
     tp.tp_token_logprobs(x[:0], tok[:0], e, e)
+
+
+# ------------------------------------------------- many rows, in 64 bits on the GPU --
+def many(n, v, dtype, seed):
+    """Rows in more rounds than the GPU has places for, a third of them padding, a few of the rest special."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    x = torch.empty((n, v), dtype=TYPES[dtype], device=DEV)
+    for a in range(0, n, 256):
+        x[a:a + 256] = torch.randn((min(256, n - a), v), generator=g, device=DEV) * 2.5
+    x[5, : v // 2] = -torch.inf
+    x[6] = -torch.inf
+    x[7, 11] = torch.nan
+    x[8] = 0.5
+    x[9, 100:] = -torch.inf
+    tok = torch.randint(0, v, (n,), generator=g, device=DEV).int()
+    tok[torch.rand(n, generator=g, device=DEV) < 0.33] = -1
+    tok[:10] = torch.arange(10, device=DEV).int()
+    return x, tok, g
+
+
+def in_parts(x, f):
+    parts = [f(x[a:a + 128].double(), slice(a, a + 128)) for a in range(0, len(x), 128)]
+    return [torch.cat(p) for p in zip(*parts)]
+
+
+@pytest.mark.parametrize("dtype,n,v", [("bf16", 1900, 40000), ("bf16", 1830, 33001), ("f32", 1850, 20001), ("bf16", 700, 150000),
+                                       ("f16", 320, 33333)])
+def test_many_rows(dtype, n, v):
+    x, tok, g = many(n, v, dtype, n + v)
+    live, at = tok >= 0, tok.long().clamp(min=0)[:, None]
+    k = 9
+
+    def exact(y, rows):
+        y = torch.where(torch.isnan(y).any(1, keepdim=True), torch.nan, y)
+        lse = torch.logsumexp(y, -1)
+        lp = y - lse[:, None]
+        lp = torch.where((lse == -torch.inf)[:, None], -torch.inf, lp)
+        p = lp.exp()
+        h = -torch.where(p > 0, p * lp, p * 0).sum(1)
+        top = torch.where(torch.isnan(lse)[:, None], torch.nan, lp.topk(k, -1).values)
+        return lp.gather(1, at[rows])[:, 0], h, lse, top
+    logp, h, lse, top = in_parts(x, exact)
+    f = lambda *s: torch.full(s, 7.0, device=DEV)  # noqa: E731
+    glp, gh, gl, ids, gtop = f(n), f(n), f(n), torch.full((n, k), -7, dtype=torch.int32, device=DEV), f(n, k)
+    tp.tp_token_logprobs(x, tok, glp, gh, gl, ids, gtop)
+    near(glp, f64(torch.where(live, logp, 0.0)), 1e-5, 2e-6, "logp")
+    near(gh, f64(torch.where(live, h, 0.0)), 3e-5, 2e-6, "entropy")
+    near(gl, f64(torch.where(live, lse, 0.0)), 1e-5, 2e-6, "lse")
+    near(gtop, f64(torch.where(live[:, None], top, -torch.inf)), 1e-5, 2e-6, "top_logp")
+    some = ids >= 0
+    assert ((ids == -1) | some).all()
+    # the ids are the places of these logits, equal ones in rising order
+    vals = x.gather(1, ids.long().clamp(min=0)).float()
+    fine = some[:, 1:] & some[:, :-1]
+    assert ((vals[:, 1:] < vals[:, :-1]) | ((vals[:, 1:] == vals[:, :-1]) & (ids[:, 1:] > ids[:, :-1])))[fine].all()
+    near(torch.where(some, vals - gl[:, None], gtop), f64(gtop), 2e-5, 4e-6, "ids")
+
+    adv, w = torch.randn(n, generator=g, device=DEV), torch.rand(n, generator=g, device=DEV) + 0.5
+    tid = torch.randint(0, v, (n, 20), generator=g, device=DEV).int()
+    tval = torch.randn((n, 20), generator=g, device=DEV)
+    tid[~live] = -1
+    beta = 0.05
+    loss, kl = f(n), f(n)
+    dp, dk = torch.empty_like(x), x.clone()
+    tp.tp_policy_loss(x, tok, adv, loss, dp, None, w, entropy_coef=beta)
+    tp.tp_distill_loss(dk, tid, tval, kl, dk, w)  # in place
+    q = torch.softmax(tval.double(), -1)
+    beta = float(np.float32(beta))
+
+    def grads(y, rows):
+        y = torch.where(torch.isnan(y).any(1, keepdim=True), torch.nan, y)
+        empty = (y == -torch.inf).all(1, keepdim=True)
+        lp = torch.where(empty, -torch.inf, y - torch.logsumexp(y, -1, keepdim=True))
+        p, l = lp.exp(), live[rows, None]
+        a, ww = -adv[rows].double()[:, None], w[rows].double()[:, None]
+        hh = torch.where(p > 0, p * lp, p * 0)
+        d = a * (torch.zeros_like(p).scatter_(1, at[rows], 1.0) - p) + beta * (hh - p * hh.sum(1, keepdim=True))
+        d = torch.where(empty, 0.0, d) * ww
+        t = torch.where(empty, 0.0, p.scatter_add(1, tid[rows].long().clamp(min=0), -q[rows])) * ww
+        d, t = torch.where(l, d, 0.0), torch.where(l, t, 0.0)
+        # half an ulp of the type, the few fp32 roundings of a row's factors, 1e-4 of a probability's share
+        u, tiny = HALF_ULP[dtype]
+        u += 5e-7
+        size = (p * (a.abs() + beta * (lp.clamp(min=-200).abs() - hh.sum(1, keepdim=True) + 1)) * ww).nan_to_num()
+        far_d = ((dp[rows].double() - d).abs() - 1.05 * u * d.abs() - 1e-4 * size - 1.01 * tiny - 1e-37)
+        far_t = ((dk[rows].double() - t).abs() - 1.05 * u * t.abs() - 1e-4 * (p * ww).nan_to_num() - 1e-6 * q[rows].amax(1, keepdim=True) * ww
+                 - 1.01 * tiny - 1e-37)
+        ok = lambda far, got, want: (torch.isnan(got) == torch.isnan(want)).all(1) & ((far <= 0) | torch.isnan(far)).all(1)  # noqa: E731
+        return ok(far_d, dp[rows], d), ok(far_t, dk[rows], t)
+    okd, okt = in_parts(x, grads)
+    assert okd.all(), torch.nonzero(~okd)[:5, 0].tolist()
+    assert okt.all(), torch.nonzero(~okt)[:5, 0].tolist()
+    want = torch.where(live, w * (-adv - beta * h), 0.0)
+    near(loss[live & ~torch.isnan(want)], f64(want[live & ~torch.isnan(want)]), 1e-4, 4e-6, "loss")
+    assert (loss[~live] == 0).all() and (kl[~live] == 0).all()
