@@ -797,10 +797,24 @@ __device__ __forceinline__ float warp_kth(float v, int at) {
     return __shfl_sync(0xffffffffu, v, at);
 }
 
-// Puts the logits of the vectors v, v + step, ... before end that are not below the bound on the list.
+// Puts the logits of vector v, r, that are not below the bound on the list.
+template <typename T>
+__device__ __forceinline__ void collect_vector(const Row<T>& row, int v, const uint4& r, float bound, Key* list, int size, int* n) {
+    constexpr int E = Vec<T>::E;
+    if (!(Vec<T>::template max_of<1>(&r) >= bound)) return;
+    float x[E];
+    Vec<T>::unpack(r, x);
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (x[e] >= bound && x[e] > kNegInf) {
+            const int at = atomicAdd(n, 1);
+            if (at < size) list[at] = make_key(x[e], v * E + e - row.lead);
+        }
+}
+
+// The same of vectors v, v + step, ... before end.
 template <typename T>
 __device__ __forceinline__ void collect(const Row<T>& row, int v, int end, int step, float bound, Key* list, int size, int* n) {
-    constexpr int E = Vec<T>::E;
     for (; v < end; v += 4 * step) {
         uint4 r[4];
 #pragma unroll
@@ -809,17 +823,7 @@ __device__ __forceinline__ void collect(const Row<T>& row, int v, int end, int s
             if (v + u * step < end) r[u] = row.load_kept(v + u * step);
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (Vec<T>::template max_of<1>(r + u) >= bound) {
-                float x[E];
-                Vec<T>::unpack(r[u], x);
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (x[e] >= bound && x[e] > kNegInf) {
-                        const int at = atomicAdd(n, 1);
-                        if (at < size) list[at] = make_key(x[e], (v + u * step) * E + e - row.lead);
-                    }
-            }
+        for (int u = 0; u < 4; ++u) collect_vector(row, v + u * step, r[u], bound, list, size, n);
     }
 }
 
@@ -1530,7 +1534,8 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
 constexpr int kNarrowWarps = 4;
 constexpr int kNarrowBytes = 32768;
 
-template <typename T, int OP, bool GRAD, bool ENT, bool TOP, int TEAM>
+// KEPT: a row has at most four vectors a thread; it is read once and stays in registers.
+template <typename T, int OP, bool GRAD, bool ENT, bool TOP, int TEAM, bool KEPT>
 __global__ void __launch_bounds__(kNarrowWarps * 32) narrow_kernel(const __grid_constant__ RowArgs a) {
     extern __shared__ __align__(16) uint8_t space[];
     constexpr int kRows = kNarrowWarps / TEAM, kTeam = TEAM * 32;
@@ -1554,38 +1559,47 @@ __global__ void __launch_bounds__(kNarrowWarps * 32) narrow_kernel(const __grid_
     const TeacherList list(space + team * list_bytes + kSeenWords * 4, a.k);
     typedef TopShared<kTeam, 1> NarrowTop;
     NarrowTop& sh = *(NarrowTop*)(space + team * (TOP ? NarrowTop::bytes(a.k, 1) : 0));
+    // whether there is anything to read; the row's own values come beside its logits, before the team meets
+    int32_t tok = 0;
+    bool live;
+    Teacher teacher;
+    float x_tok = NAN, w = 1.f, adv = 0.f, old = 0.f;
     if constexpr (OP == OP_DISTILL) {
-        if (t < 32) {
-            for (int k = lane; k < kSeenWords; k += 32) seen[k] = 0;
-            __syncwarp();
-            const Teacher teacher = teacher_first(a, i);
-            if (lane == 0) info.live = teacher.live;
-            teacher_rest(a, i, teacher, row, 0, row.n_vec, 0, info, list, seen);
-        }
-    } else if (t == 0) {
-        const int32_t tok = a.tokens ? a.tokens[i] : 0;
-        info.tok = tok;
-        info.live = tok >= 0;
-        info.x_tok = a.tokens && tok >= 0 && tok < a.vocab ? to_f32(row.x[tok]) : NAN;  // (before a gradient in place)
-        info.w = a.weight ? a.weight[i] : 1.f;
-        if (OP == OP_POLICY) {
-            info.adv = a.advantage[i];
-            info.old = a.old_logp ? a.old_logp[i] : 0.f;
+        teacher = teacher_first(a, i);
+        live = teacher.live;
+    } else {
+        if (a.tokens) tok = a.tokens[i];
+        live = tok >= 0;
+        if (t == 0) {
+            if (a.tokens && live && tok < a.vocab) x_tok = to_f32(row.x[tok]);
+            if (OP == OP_POLICY) {
+                w = a.weight ? a.weight[i] : 1.f;
+                adv = a.advantage[i];
+                old = a.old_logp ? a.old_logp[i] : 0.f;
+            }
         }
     }
-    if constexpr (TOP)
-        if (t == 0) sh.n[0] = 0;
-    sync();
-    // f(Count<M>, M vectors kTeam apart, the first's number) over the row; the warp's lanes together, a vector past the end is -inf
+    // f(Count<M>, M vectors kTeam apart, the first's number) over the row; the warp's lanes together, a vector past the
+    // end is -inf.
+    uint4 r0[KEPT ? 4 : 1];
+    auto load4 = [&](uint4* r, int g) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            r[u] = make_uint4(Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone);
+            if (g + u * kTeam + lane < row.n_vec) r[u] = row.load_kept(g + u * kTeam + lane);
+        }
+    };
+    if constexpr (KEPT)
+        if (live) load4(r0, t - lane);
     auto each = [&](auto f) {
+        if constexpr (KEPT) {
+            f(Count<4>{}, r0, t);
+            return;
+        }
         int g = t - lane;
         for (; g + 3 * kTeam < row.n_vec; g += 4 * kTeam) {
             uint4 r[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                r[u] = make_uint4(Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone);
-                if (g + u * kTeam + lane < row.n_vec) r[u] = row.load_kept(g + u * kTeam + lane);
-            }
+            load4(r, g);
             f(Count<4>{}, r, g + lane);
         }
         for (; g < row.n_vec; g += kTeam) {
@@ -1594,13 +1608,29 @@ __global__ void __launch_bounds__(kNarrowWarps * 32) narrow_kernel(const __grid_
             f(Count<1>{}, &r, g + lane);
         }
     };
+    if constexpr (OP == OP_DISTILL) {
+        if (t < 32) {
+            for (int k = lane; k < kSeenWords; k += 32) seen[k] = 0;
+            __syncwarp();
+            teacher_rest(a, i, teacher, row, 0, row.n_vec, 0, info, list, seen);
+        }
+    }
     Running run;
-    const bool live = info.live;
     if (live) each([&](auto count, const uint4* r, int) { run.add<T, ENT, decltype(count)::n>(r, c); });
+    if (OP != OP_DISTILL && t == 0) {
+        info.tok = tok;
+        info.x_tok = x_tok;  // (read before a gradient in place)
+        info.w = w;
+        info.adv = adv;
+        info.old = old;
+    }
+    if (TOP && t == 0) sh.n[0] = 0;
     Stats all = run.stats();
     all.join_warp<ENT>(c);
     bool low = GRAD && ENT && __any_sync(0xffffffffu, run.low);
-    if constexpr (TEAM > 1) {
+    if constexpr (TEAM == 1) {
+        __syncwarp();
+    } else {
         if (lane == 0) parts[warp] = make_float4(all.m, all.s, all.t, low ? 1.f : 0.f);
         if constexpr (TOP) sh.most[0][t] = run.m;
         sync();
@@ -1641,7 +1671,13 @@ __global__ void __launch_bounds__(kNarrowWarps * 32) narrow_kernel(const __grid_
             else if (a.k <= 32)
                 bound = warp_kth(run.m, a.k - 1);
             const int size = NarrowTop::list_size(a.k);
-            if (run.m >= bound) collect(row, t, row.n_vec, kTeam, bound, keys, size, &sh.n[0]);
+            if (run.m >= bound) {
+                if constexpr (KEPT)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) collect_vector(row, t + u * kTeam, r0[u], bound, keys, size, &sh.n[0]);
+                else
+                    collect(row, t, row.n_vec, kTeam, bound, keys, size, &sh.n[0]);
+            }
             sync();
             if (sh.n[0] > size) {
                 sync();
@@ -1810,15 +1846,21 @@ cudaError_t launch_narrow(const RowArgs& a, cudaStream_t s) {
     constexpr int kRows = kNarrowWarps / TEAM;
     const int bytes = TOP ? kRows * TopShared<TEAM * 32, 1>::bytes(a.k, 1) : OP == OP_DISTILL ? kRows * (kSeenWords * 4 + a.k * TeacherList::kBytes) : 0;
     static_assert(kNarrowWarps * (kSeenWords * 4 + TP_MAX_TEACHER_LOGITS * TeacherList::kBytes) + 1024 <= 48 * 1024);
-    return launch_kernel(narrow_kernel<T, OP, GRAD, ENT, TOP, TEAM>, (a.n + (int64_t)kRows - 1) / kRows, 0, true, kNarrowWarps * 32, bytes, s, a);
+    constexpr int E = Vec<T>::E;
+    const bool kept = (GRAD || TOP) && (a.vocab + 2 * E - 2) / E <= 4 * TEAM * 32;
+    return launch_kernel(kept ? narrow_kernel<T, OP, GRAD, ENT, TOP, TEAM, GRAD || TOP> : narrow_kernel<T, OP, GRAD, ENT, TOP, TEAM, false>, (a.n + (int64_t)kRows - 1) / kRows, 0, true, kNarrowWarps * 32, bytes, s, a);
 }
 
 template <typename T, int OP, bool GRAD, bool ENT, bool TOP = false>
 cudaError_t launch_rows(const RowArgs& a, cudaStream_t s) {
     constexpr int E = Vec<T>::E;
     if ((int64_t)a.vocab * (int)sizeof(T) <= kNarrowBytes) {
-        // one warp a row where it has at most four vectors for a lane and there are enough rows to fill the GPU
-        if (a.vocab * (int)sizeof(T) <= 2048 && a.n >= 2048 && (!TOP || a.k <= 32)) return launch_narrow<T, OP, GRAD, ENT, TOP, 1>(a, s);
+        // One warp a row where it holds the row, or where there are rows enough for 32 warps an SM (us, one warp / four:
+        // policy loss of 8192 rows of 8 KB 32 / 38, of 2500 15 / 12, distillation 44 / 52, 22 / 15); a warp's lanes give
+        // a bound for up to 32 alternatives.
+        const int bytes = a.vocab * (int)sizeof(T);
+        if ((bytes <= 2048 ? a.n >= 2048 : bytes <= (TOP ? 16384 : 8192) && a.n >= 4864) && (!TOP || a.k <= 32))
+            return launch_narrow<T, OP, GRAD, ENT, TOP, 1>(a, s);
         return launch_narrow<T, OP, GRAD, ENT, TOP, kNarrowWarps>(a, s);
     }
     // (rows that all begin in a line of their own have one vector less than rows at any place)
