@@ -50,6 +50,7 @@ constexpr uint64_t kWaitLimitNs = 2000000000ull;  // bounded waits: 2 s
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNegInf = -INFINITY;
+constexpr float kFar = -256.f;       // 2^x (and e^x) is 0 here and below: where x is a factor beside it, this will do
 
 // ------------------------------------------------------------------ pieces --
 __device__ __forceinline__ float exp2_approx(float x) {  // 2 ulp; exp2(-inf) = +0
@@ -448,7 +449,7 @@ struct Stats {
     __device__ __forceinline__ void join_warp(float c) {
         const float most = warp_max(m);
         const float d = m == kNegInf ? 0.f : c * (m - most), f = m == kNegInf ? 0.f : exp2_approx(d);
-        if (ENT) t = warp_sum(f * (t + s * fmaxf(d, -1e30f)));
+        if (ENT) t = warp_sum(f * (t + s * fmaxf(d, kFar)));
         s = warp_sum(f * s);
         m = most;
     }
@@ -463,7 +464,7 @@ struct Running {
     bool low = false;
 
     __device__ __forceinline__ void raise(float m2, float c) {  // m2 > m
-        const float d = m == kNegInf ? 0.f : fmaxf(c * (m - m2), -1e30f), f = m == kNegInf ? 0.f : exp2_approx(d);
+        const float d = m == kNegInf ? 0.f : fmaxf(c * (m - m2), kFar), f = m == kNegInf ? 0.f : exp2_approx(d);
         const F2 d2(d, d), f2(f, f);
         t = f2 * fma2(s, d2, t);
         s = f2 * s;
@@ -503,7 +504,7 @@ struct Running {
 #pragma unroll
                     for (int e = 0; e < Vec<T>::E / 2; ++e) {
                         d[e] = (d[e] * c2);
-                        part = fma2(exp2_of(d[e]), d[e].at_least(-1e30f), part);
+                        part = fma2(exp2_of(d[e]), d[e].at_least(kFar), part);
                     }
                 }
             }
@@ -571,7 +572,7 @@ struct RowInfo {
 struct Coef {
     float m, log2_s, k0, k1, k2;
     int32_t terms;  // whether tokens have terms of their own
-    int32_t low;    // whether log2 p may be infinite where p = 0
+    int32_t low;    // whether k1 log2 p may be infinite where p = 0
 };
 
 template <typename T>
@@ -595,7 +596,6 @@ __device__ __forceinline__ Coef coefficients(const RowArgs& a, const RowInfo<T>&
     Coef f{};
     f.m = res.m;
     f.log2_s = res.log2_s;
-    f.low = low;
     logp = NAN;
     if (OP != OP_DISTILL && info.tok < a.vocab) logp = res.logp(info.x_tok);
     if constexpr (OP == OP_POLICY) {
@@ -605,6 +605,7 @@ __device__ __forceinline__ Coef coefficients(const RowArgs& a, const RowInfo<T>&
         f.k0 = wt * (ENT ? a.entropy_coef * res.entropy - g : -g);
         f.k1 = ENT ? wt * a.entropy_coef * kLn2 : 0.f;
         f.k2 = wt * g;
+        f.low = low || !(fabsf(f.k1) < 1.f);
         f.terms = info.tok < a.vocab && !res.empty;
     }
     if constexpr (OP == OP_DISTILL) {
@@ -635,7 +636,7 @@ __device__ __forceinline__ uint4 gradient(const uint4& r, const Coef& f, float c
     for (int e = 0; e < E / 2; ++e) {
         d[e] = fma2(d[e], c2, less);
         const F2 p = exp2_of(d[e]);
-        if (ENT && low) d[e] = d[e].at_least(-1e30f);
+        if (ENT && low) d[e] = d[e].at_least(kFar);
         (p * (ENT ? fma2(k1, d[e], k0) : k0)).get(y[2 * e], y[2 * e + 1]);
     }
     return Vec<T>::pack(y);
@@ -663,7 +664,7 @@ __device__ __forceinline__ void own_terms(const Row<T>& row, const RowInfo<T>& i
     if constexpr (OP == OP_POLICY) {
         if (lane == 0 && mine(info.tok)) {
             const float d = fmaf(c, info.x_tok - f.m, -f.log2_s), p = exp2_approx(d);
-            row.dx[info.tok] = from_f32<T>(fmaf(p, ENT ? fmaf(f.k1, fmaxf(d, -1e30f), f.k0) : f.k0, f.k2));
+            row.dx[info.tok] = from_f32<T>(fmaf(p, ENT ? fmaf(f.k1, fmaxf(d, kFar), f.k0) : f.k0, f.k2));
         }
     }
     if constexpr (OP == OP_DISTILL) {
@@ -1330,7 +1331,7 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
 #pragma unroll
             for (int k = 0; k < kMost; ++k) {
                 const float d = p[k].x == kNegInf ? 0.f : c * (p[k].x - all.m), f = p[k].x == kNegInf ? 0.f : exp2_approx(d);
-                if (ENT) all.t += f * (p[k].z + p[k].y * fmaxf(d, -1e30f));
+                if (ENT) all.t += f * (p[k].z + p[k].y * fmaxf(d, kFar));
                 all.s += f * p[k].y;
             }
             all.s = warp_sum(all.s);
@@ -1744,7 +1745,7 @@ __global__ void __launch_bounds__(kBackThreads) backward_kernel(const __grid_con
             lp.get(l0, l1);
             (lp * F2(kLog2e, kLog2e)).get(d0, d1);
             const F2 p(exp2_approx(d0), exp2_approx(d1));
-            (p * (ENT ? fma2(F2(k1, k1), F2(fmaxf(l0, -1e30f), fmaxf(l1, -1e30f)), F2(k0, k0)) : F2(k0, k0))).get(x[e], x[e + 1]);
+            (p * (ENT ? fma2(F2(k1, k1), F2(fmaxf(l0, kFar), fmaxf(l1, kFar)), F2(k0, k0)) : F2(k0, k0))).get(x[e], x[e + 1]);
         }
         if (v == tok_vec) {
             const int at = (tok + row.lead) % E;

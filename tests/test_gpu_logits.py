@@ -296,6 +296,21 @@ def test_special_rows(dtype, v, temperature):
         check_distill(x, ids, teacher, None, dtype, temperature)
 
 
+# masks by finite values that stay finite as x / T, with coefficients that take their product past fp32
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,v", [(3, 700), (2100, 300), (3, 9001), (3, 40000)])
+def test_far_masks_and_large_coefficients(dtype, n, v):
+    x, tok, g = make(n, v, dtype)
+    a = torch.randn(n, generator=g, device=DEV)
+    for mask in (-3e38, -1e30, -np.inf):
+        x[:, v // 2:] = mask
+        x[:, v // 3] = -3e38
+        tok[0], tok[1] = v // 2 - 1, v - 1
+        check_policy(x, tok, a, None, None, dtype, 2.0, beta=8.0)
+        check_policy(x, tok, a, None, torch.full((n,), 1e4, device=DEV), dtype, 2.0)
+        check_backward(x, tok, a, 1e9 * (a.abs() + 1), dtype, 2.0)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_tokens_out_of_range_and_padding(dtype):
     v = 5000
