@@ -1701,7 +1701,7 @@ __global__ void __launch_bounds__(kBackThreads) backward_kernel(const __grid_con
     constexpr int E = Vec<T>::E;
     after_predecessor();
     constexpr int kUnit = WARPS ? 32 : kBackThreads;  // threads, and vectors between a thread's
-    const uint32_t unit = WARPS ? (blockIdx.x * kBackThreads + threadIdx.x) / 32 : blockIdx.x;
+    const uint32_t unit = WARPS ? blockIdx.x * (kBackThreads / 32) + threadIdx.x / 32 : blockIdx.x;
     if (unit >= units) return;
     const int64_t i = unit / units_per_row;
     const int first = (int)(unit - (uint32_t)i * units_per_row) * kUnit * kBackVecs + threadIdx.x % kUnit;
