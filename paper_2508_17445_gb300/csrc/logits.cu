@@ -705,10 +705,10 @@ __device__ __forceinline__ float teacher_loss(const TeacherList& list, int k, co
 // finding the k-th largest key by its digits.
 constexpr int kCells = 8;
 constexpr int kPlaces = 512;
-template <int THREADS, int SLOTS>
+template <int THREADS, int SLOTS, int CELLS = 1>
 struct TopShared {
     uint64_t best_full[SLOTS];
-    float most[SLOTS][THREADS];                   // the threads' largest logits
+    float most[SLOTS][CELLS * THREADS];           // the threads' largest logits (short rows: of either half of their vectors)
     __nv_bfloat16 part[SLOTS][kCells][THREADS];   // of the parts, rounded up
     uint16_t place[SLOTS][kPlaces];               // thread and part that are read again
     int n[SLOTS];                                 // keys on the list
@@ -716,7 +716,7 @@ struct TopShared {
     // behind it: the slots' lists of list_size(k) keys, then the first CTA's best keys of each slot and CTA: k, descending,
     // 0 where none is left
 
-    static __host__ __device__ __forceinline__ int list_size(int k) { return 4 * k + 64; }
+    static __host__ __device__ __forceinline__ int list_size(int k) { return 2 * k + 64; }
     static __host__ __device__ __forceinline__ int bytes(int k, int cta_n) {
         return (int)sizeof(TopShared) + SLOTS * 8 * (list_size(k) + (cta_n > 1 ? cta_n * k : 0));
     }
@@ -813,19 +813,63 @@ __device__ __forceinline__ void collect_vector(const Row<T>& row, int v, const u
         }
 }
 
-// The same of vectors v, v + step, ... before end.
-template <typename T>
-__device__ __forceinline__ void collect(const Row<T>& row, int v, int end, int step, float bound, Key* list, int size, int* n) {
-    for (; v < end; v += 4 * step) {
-        uint4 r[4];
+// A list for vectors first .. first + n - 1, which hold too many logits of at least b, from memory, by THREADS threads:
+// the bound is raised to a value that k of them and few more are not below, by halving between b and the largest, in
+// turn of the values and of the keys. False: there is none (equal logits), or fewer than k.
+template <int THREADS, typename T, typename S>
+__device__ __noinline__ bool collect_raised(const Row<T>& row, int first, int n, int k, float b, float most, S& sh, int s) {
+    constexpr int E = Vec<T>::E;
+    const int t = threadIdx.x % THREADS, size = S::list_size(k);
+    auto each_vec = [&](auto f) {
+        for (int v = first + t; v < first + n; v += 4 * THREADS) {
+            uint4 r[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            r[u] = make_uint4(Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone);
-            if (v + u * step < end) r[u] = row.load_kept(v + u * step);
+            for (int u = 0; u < 4; ++u) {
+                r[u] = make_uint4(Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone);
+                if (v + u * THREADS < first + n) r[u] = row.load_kept(v + u * THREADS);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) f(r[u], v + u * THREADS);
         }
+    };
+    auto order = [](float x) { return (uint32_t)(make_key(x, 0) >> 32); };
+    uint32_t lo = order(b), hi = order(most) + 1;
+    for (int round = 0; hi - lo > 1; ++round) {
+        uint32_t mid = lo + (hi - lo) / 2;
+        if (round % 2 == 0) {
+            const uint32_t m = order(0.5f * key_value((Key)lo << 32) + 0.5f * key_value((Key)(hi - 1) << 32));
+            if (m > lo && m < hi) mid = m;
+        }
+        const float x = key_value((Key)mid << 32);
+        int c = 0;
+        each_vec([&](const uint4& r, int) {
+            if (!(Vec<T>::template max_of<1>(&r) >= x)) return;
+            float f[E];
+            Vec<T>::unpack(r, f);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) collect_vector(row, v + u * step, r[u], bound, list, size, n);
+            for (int e = 0; e < E; ++e) c += f[e] >= x;
+        });
+        c = __reduce_add_sync(0xffffffffu, c);
+        if constexpr (THREADS > 32) {
+            if (t % 32 == 0) sh.hist[s][t / 32] = c;
+            threads_sync<THREADS>();
+            c = 0;
+            for (int w = 0; w < THREADS / 32; ++w) c += sh.hist[s][w];
+            threads_sync<THREADS>();
+        }
+        if (c < k) {
+            hi = mid;
+        } else if (c > k + k / 4 + 16) {
+            lo = mid;
+        } else {
+            if (t == 0) sh.n[s] = 0;
+            threads_sync<THREADS>();
+            each_vec([&](const uint4& r, int v) { collect_vector(row, v, r, x, sh.list(s, k), size, &sh.n[s]); });
+            threads_sync<THREADS>();
+            return true;
+        }
     }
+    return false;
 }
 
 // The list of the slice's k largest keys (it has more), from memory, by THREADS
@@ -936,7 +980,8 @@ __device__ __forceinline__ float kth_of_maxima(const float* most, int k, float b
 
 // One helper warp: the list of what is not below the bound, from the working threads' parts of the slice.
 template <typename T>
-__device__ __forceinline__ void collect_parts(const Row<T>& row, int first, int n, int chunk, int k, float bound, WideTop& sh, int s) {
+__device__ __forceinline__ void collect_parts(const Row<T>& row, int first, int n, int chunk, int k, float bound, float row_most, WideTop& sh,
+                                              int s) {
     const int lane = threadIdx.x & 31, chunks = (n + chunk - 1) / chunk, per_part = (chunks + kCells - 1) / kCells;
     Key* list = sh.list(s, k);
     int m = 0;
@@ -993,14 +1038,15 @@ __device__ __forceinline__ void collect_parts(const Row<T>& row, int first, int 
                 }
         }
     __syncwarp();
-    if (m > kPlaces || hits > kHits || sh.n[s] > WideTop::list_size(k)) collect_exact<32>(row, first, n, k, sh, s);
+    if ((m > kPlaces || hits > kHits || sh.n[s] > WideTop::list_size(k)) && !collect_raised<32>(row, first, n, k, bound, row_most, sh, s))
+        collect_exact<32>(row, first, n, k, sh, s);
 }
 
-// One helper warp: the row's alternatives from the CTAs' lists.
-template <typename S>
+// The row's alternatives from the CTAs' lists; one helper warp, or a short row's team (threads t of THREADS).
+template <int THREADS, typename S>
 __device__ __forceinline__ void alternatives(const RowArgs& a, int64_t i, S& sh, int s, uint32_t parity, uint32_t rank, int cta_n,
                                              const RowResult& r, volatile int* dead) {
-    const int lane = threadIdx.x & 31, k = a.k;
+    const int lane = threadIdx.x & 31, t = threadIdx.x % THREADS, k = a.k;
     Key* list = sh.list(s, k);
     const int m = min(sh.n[s], S::list_size(k));
     const bool nan = isnan(r.lse), alone = cta_n == 1;
@@ -1011,7 +1057,7 @@ __device__ __forceinline__ void alternatives(const RowArgs& a, int64_t i, S& sh,
     };
     const uint32_t bar = map_to(smem_addr(&sh.best_full[s]), 0), dst = map_to(smem_addr(sh.best(s, rank, k, cta_n)), 0);
     if (!alone && rank == 0 && lane == 0) mbar_expect(smem_addr(&sh.best_full[s]), cta_n * k * 8);
-    for (int p = lane; p < max(m, k); p += 32) {
+    for (int p = t; p < max(m, k); p += THREADS) {
         const Key key = p < m ? list[p] : 0;
         int place = p;
         if (p < m) {
@@ -1358,8 +1404,8 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
                 if (rank == 0) write_results<OP, ENT>(a, i, live, info.w, res, logp, term);
             }
             if constexpr (TOP) {
-                if (live) collect_parts(row, first, max(0, min(plan.per_cta, row.n_vec - first)), plan.chunk, a.k, bound, sh, s);
-                alternatives(a, i, sh, s, parity_of(q), rank, cta_n, res, &sm.dead);
+                if (live) collect_parts(row, first, max(0, min(plan.per_cta, row.n_vec - first)), plan.chunk, a.k, bound, res.m, sh, s);
+                alternatives<32>(a, i, sh, s, parity_of(q), rank, cta_n, res, &sm.dead);
             }
             if (OP == OP_DISTILL && rank == 0) {
                 const float loss = live && !info.bad ? teacher_loss(list_at(s), a.k, res) : 0.f;
@@ -1534,6 +1580,7 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
 // 1 us of a CTA: helpers, barriers, exchange) would be most of a short row's time.
 constexpr int kNarrowWarps = 4;
 constexpr int kNarrowBytes = 32768;
+constexpr int kAloneTop = 24;  // alternatives that one warp's lanes give a bound for
 
 // KEPT: a row has at most four vectors a thread; it is read once and stays in registers.
 template <typename T, int OP, bool GRAD, bool ENT, bool TOP, int TEAM, bool KEPT>
@@ -1558,7 +1605,7 @@ __global__ void __launch_bounds__(kNarrowWarps * 32) narrow_kernel(const __grid_
     const int list_bytes = kSeenWords * 4 + a.k * TeacherList::kBytes;
     uint32_t* seen = (uint32_t*)(space + team * list_bytes);
     const TeacherList list(space + team * list_bytes + kSeenWords * 4, a.k);
-    typedef TopShared<kTeam, 1> NarrowTop;
+    typedef TopShared<kTeam, 1, 2> NarrowTop;
     NarrowTop& sh = *(NarrowTop*)(space + team * (TOP ? NarrowTop::bytes(a.k, 1) : 0));
     // whether there is anything to read; the row's own values come beside its logits, before the team meets
     int32_t tok = 0;
@@ -1617,7 +1664,23 @@ __global__ void __launch_bounds__(kNarrowWarps * 32) narrow_kernel(const __grid_
         }
     }
     Running run;
-    if (live) each([&](auto count, const uint4* r, int) { run.add<T, ENT, decltype(count)::n>(r, c); });
+    const bool halves = TOP && TEAM > 1 && a.k > kTeam / 2;
+    float most0 = kNegInf, most1 = kNegInf;  // of the vectors' halves
+    if (live) {
+        if (halves)
+            each([&](auto count, const uint4* r, int) {
+                constexpr int N = decltype(count)::n;
+                run.add<T, ENT, N>(r, c);
+#pragma unroll
+                for (int u = 0; u < N; ++u) {
+                    const uint4 lo = make_uint4(r[u].x, r[u].y, r[u].x, r[u].y), hi = make_uint4(r[u].z, r[u].w, r[u].z, r[u].w);
+                    most0 = fmaxf(most0, Vec<T>::template max_of<1>(&lo));
+                    most1 = fmaxf(most1, Vec<T>::template max_of<1>(&hi));
+                }
+            });
+        else
+            each([&](auto count, const uint4* r, int) { run.add<T, ENT, decltype(count)::n>(r, c); });
+    }
     if (OP != OP_DISTILL && t == 0) {
         info.tok = tok;
         info.x_tok = x_tok;  // (read before a gradient in place)
@@ -1626,14 +1689,19 @@ __global__ void __launch_bounds__(kNarrowWarps * 32) narrow_kernel(const __grid_
         info.old = old;
     }
     if (TOP && t == 0) sh.n[0] = 0;
+    float least = kNegInf;
+    if (TOP && TEAM > 1) least = warp_kth(run.m, (a.k + TEAM - 1) / TEAM - 1);
     Stats all = run.stats();
     all.join_warp<ENT>(c);
     bool low = GRAD && ENT && __any_sync(0xffffffffu, run.low);
     if constexpr (TEAM == 1) {
         __syncwarp();
     } else {
-        if (lane == 0) parts[warp] = make_float4(all.m, all.s, all.t, low ? 1.f : 0.f);
-        if constexpr (TOP) sh.most[0][t] = run.m;
+        if (lane == 0) parts[warp] = make_float4(all.m, all.s, all.t, TOP ? least : low ? 1.f : 0.f);
+        if constexpr (TOP) {
+            sh.most[0][t] = halves ? most0 : run.m;
+            if (halves) sh.most[0][kTeam + t] = most1;
+        }
         sync();
         const float4 p = parts[lane % TEAM];
         all.m = p.x, all.s = lane < TEAM ? p.y : 0.f, all.t = lane < TEAM ? p.z : 0.f;
@@ -1667,25 +1735,42 @@ __global__ void __launch_bounds__(kNarrowWarps * 32) narrow_kernel(const __grid_
         Key* keys = sh.list(0, a.k);
         if (live) {
             float bound = kNegInf;
-            if constexpr (TEAM > 1)
-                bound = kth_of_maxima<kTeam>(sh.most[0], a.k, kNegInf);
-            else if (a.k <= 32)
+            if constexpr (TEAM > 1) {
+                const float b = fminf(fminf(parts[0].w, parts[1].w), fminf(parts[2].w, parts[3].w));
+                bound = halves ? kth_of_maxima<2 * kTeam>(sh.most[0], a.k, b) : kth_of_maxima<kTeam>(sh.most[0], a.k, b);
+            } else {
                 bound = warp_kth(run.m, a.k - 1);
+            }
             const int size = NarrowTop::list_size(a.k);
-            if (run.m >= bound) {
-                if constexpr (KEPT)
+            // the warp's vectors that hold such logits, then their logits, a vector a lane
+            constexpr int kHits = kPlaces / TEAM;
+            uint16_t* hit_vec = sh.place[0] + warp % TEAM * kHits;
+            int hits = 0;
+            if (__any_sync(0xffffffffu, run.m >= bound))
+                each([&](auto count, const uint4* r, int v) {
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) collect_vector(row, t + u * kTeam, r0[u], bound, keys, size, &sh.n[0]);
-                else
-                    collect(row, t, row.n_vec, kTeam, bound, keys, size, &sh.n[0]);
+                    for (int u = 0; u < decltype(count)::n; ++u) {
+                        const float most = Vec<T>::template max_of<1>(r + u);
+                        const bool hit = most >= bound && most > kNegInf;
+                        const uint32_t who = __ballot_sync(0xffffffffu, hit);
+                        const int at = hits + __popc(who & ((1u << lane) - 1));
+                        if (hit && at < kHits) hit_vec[at] = (uint16_t)(v + u * kTeam);
+                        hits += __popc(who);
+                    }
+                });
+            __syncwarp();
+            if (hits > kHits) {
+                if (lane == 0) atomicAdd(&sh.n[0], size + 1);
+            } else {
+                for (int h = lane; h < hits; h += 32) collect_vector(row, hit_vec[h], row.load_kept(hit_vec[h]), bound, keys, size, &sh.n[0]);
             }
             sync();
             if (sh.n[0] > size) {
                 sync();
-                collect_exact<kTeam>(row, 0, row.n_vec, a.k, sh, 0);
+                if (!collect_raised<kTeam>(row, 0, row.n_vec, a.k, bound, res.m, sh, 0)) collect_exact<kTeam>(row, 0, row.n_vec, a.k, sh, 0);
             }
         }
-        if (t < 32) alternatives(a, i, sh, 0, 0, 0, 1, res, nullptr);
+        alternatives<kTeam>(a, i, sh, 0, 0, 0, 1, res, nullptr);
     }
 }
 
@@ -1845,7 +1930,7 @@ bool make_launch(const Shape& h, Launch& out) {
 template <typename T, int OP, bool GRAD, bool ENT, bool TOP, int TEAM>
 cudaError_t launch_narrow(const RowArgs& a, cudaStream_t s) {
     constexpr int kRows = kNarrowWarps / TEAM;
-    const int bytes = TOP ? kRows * TopShared<TEAM * 32, 1>::bytes(a.k, 1) : OP == OP_DISTILL ? kRows * (kSeenWords * 4 + a.k * TeacherList::kBytes) : 0;
+    const int bytes = TOP ? kRows * TopShared<TEAM * 32, 1, 2>::bytes(a.k, 1) : OP == OP_DISTILL ? kRows * (kSeenWords * 4 + a.k * TeacherList::kBytes) : 0;
     static_assert(kNarrowWarps * (kSeenWords * 4 + TP_MAX_TEACHER_LOGITS * TeacherList::kBytes) + 1024 <= 48 * 1024);
     constexpr int E = Vec<T>::E;
     const bool kept = (GRAD || TOP) && (a.vocab + 2 * E - 2) / E <= 4 * TEAM * 32;
@@ -1857,10 +1942,10 @@ cudaError_t launch_rows(const RowArgs& a, cudaStream_t s) {
     constexpr int E = Vec<T>::E;
     if ((int64_t)a.vocab * (int)sizeof(T) <= kNarrowBytes) {
         // One warp a row where it holds the row, or where there are rows enough for 32 warps an SM (us, one warp / four:
-        // policy loss of 8192 rows of 8 KB 32 / 38, of 2500 15 / 12, distillation 44 / 52, 22 / 15); a warp's lanes give
-        // a bound for up to 32 alternatives.
+        // policy loss of 8192 rows of 8 KB 32 / 38, of 2500 15 / 12, distillation 44 / 52, 22 / 15). The bound of a warp's
+        // lanes is too low for more than kAloneTop alternatives (8192x2000 fp32, 24: 27 / 34; 8192x4000 bf16, 32: 84 / 43).
         const int bytes = a.vocab * (int)sizeof(T);
-        if ((bytes <= 2048 ? a.n >= 2048 : bytes <= (TOP ? 16384 : 8192) && a.n >= 4864) && (!TOP || a.k <= 32))
+        if ((bytes <= 2048 ? a.n >= 2048 : bytes <= (TOP ? 16384 : 8192) && a.n >= 4864) && (!TOP || a.k <= kAloneTop))
             return launch_narrow<T, OP, GRAD, ENT, TOP, 1>(a, s);
         return launch_narrow<T, OP, GRAD, ENT, TOP, kNarrowWarps>(a, s);
     }

@@ -296,6 +296,18 @@ def test_special_rows(dtype, v, temperature):
         check_distill(x, ids, teacher, None, dtype, temperature)
 
 
+# the largest logits beside one another, where few threads meet them; rows in which nearly all are alternatives
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,v", [(6, 130), (6, 1000), (5000, 300), (6, 9001), (6, 40009), (6, 131072)])
+def test_alternatives_in_one_place(dtype, n, v):
+    x, tok, _ = make(n, v, dtype, 1)
+    for i, (at, wide) in enumerate([(0, 40), (v // 2, 200), (v - 100, 100), (v // 3, v // 3)]):
+        x[i, max(at, 0):at + wide] += 25
+    x[4, 60:] = -np.inf
+    for k in (1, 24, 25, 65, 128):
+        check_logprobs(x, tok, k)
+
+
 # masks by finite values that stay finite as x / T, with coefficients that take their product past fp32
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n,v", [(3, 700), (2100, 300), (3, 9001), (3, 40000)])
