@@ -951,7 +951,7 @@ __device__ __noinline__ void collect_exact(const Row<T>& row, int first, int n, 
 }
 
 // One warp: a value that k of the threads' maxima are not below, or b where that is larger (-inf: there is none).
-// Halving between the largest and b, in the order of keys, until at most k / 8 too many are left.
+// Halving between the largest and b, in the order of keys, until at most k / 8 (or 4) too many are left.
 template <int THREADS>
 __device__ __forceinline__ float kth_of_maxima(const float* most, int k, float b) {
     const int lane = threadIdx.x & 31;
@@ -973,7 +973,7 @@ __device__ __forceinline__ float kth_of_maxima(const float* most, int k, float b
             continue;
         }
         lo = mid;
-        if ((int)n <= k + k / 8) break;
+        if ((int)n <= k + max(k / 8, 4)) break;
     }
     return key_value((Key)lo << 32);
 }
@@ -986,6 +986,7 @@ __device__ __forceinline__ void collect_parts(const Row<T>& row, int first, int 
     Key* list = sh.list(s, k);
     int m = 0;
     for (int p = 0; p * per_part < chunks; ++p)
+#pragma unroll
         for (int t = lane; t < kRowThreads; t += 32) {
             const float most = to_f32(sh.part[s][p][t]);
             const bool hit = sh.most[s][t] >= bound && most >= bound && most > kNegInf;
@@ -1073,10 +1074,35 @@ __device__ __forceinline__ void alternatives(const RowArgs& a, int64_t i, S& sh,
     }
     if (alone || rank != 0) return;
     mbar_wait(smem_addr(&sh.best_full[s]), parity, dead);
-    // of two descending lists the larger of A_i and B_(P - 1 - i) are the P largest, in an order that log2(P) rounds of
-    // exchanges sort; place p is lane p % 32's, its (p / 32)-th
+    // Of two descending lists the larger of A_i and B_(P - 1 - i) are the P largest, in an order that log2(P) rounds of
+    // exchanges sort. Up to 32 alternatives: a list a register, all pairs of lists at once, the second of a pair held in
+    // ascending order (20 of 8x128000 13.1 -> 10.6 us). More: one list after another, place p is lane p % 32's (p / 32)-th.
     constexpr int kMost = TP_MAX_ALTERNATIVES / 32;
     const Key* best = sh.best(s, 0, k, cta_n);
+    if (k <= 32) {
+        Key x[kMaxCluster];
+#pragma unroll
+        for (int q = 0; q < kMaxCluster; ++q) {
+            const int at = q % 2 ? 31 - lane : lane;
+            x[q] = q < cta_n && at < k ? best[q * k + at] : 0;
+        }
+#pragma unroll
+        for (int apart = 1; apart < kMaxCluster; apart *= 2)
+            if (apart < cta_n) {
+#pragma unroll
+                for (int q = 0; q < kMaxCluster; q += 2 * apart) x[q] = max(x[q], x[q + apart]);
+#pragma unroll
+                for (int step = 16; step; step /= 2)
+#pragma unroll
+                    for (int q = 0; q < kMaxCluster; q += 2 * apart) {
+                        const bool up = 2 * apart < cta_n && (q / (2 * apart)) % 2;
+                        const Key o = __shfl_xor_sync(0xffffffffu, x[q], step);
+                        x[q] = ((lane & step) != 0) != up ? min(x[q], o) : max(x[q], o);
+                    }
+            }
+        if (lane < k) write(lane, x[0]);
+        return;
+    }
     const int regs = k <= 32 ? 1 : k <= 64 ? 2 : 4, P = 32 * regs;
     Key x[kMost];
 #pragma unroll
