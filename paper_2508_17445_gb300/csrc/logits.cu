@@ -8,15 +8,10 @@
 // would overflow in c x_j, and the row's largest terms lose nothing.
 //
 // All of it is bound by HBM: 8 to 20 operations an element against its 2 or 4
-// bytes. wide_kernel is persistent: a cluster of CTAs takes row after row, each CTA
-// a slice of it, which bulk copies bring chunk by chunk through a ring in shared
-// memory. Eight warps take the slice's statistics and send them to every CTA of the
-// cluster through distributed shared memory. A helper warp, which had looked up the
-// row's own values before its turn, joins them, writes the row's results and leaves
-// the gradient's coefficients; for the gradient the slice comes through the ring
-// once more, from L2, which holds the rows at work. So HBM reads a row once, the
-// whole ring is ahead of the work, and nothing waits for a whole CTA.
-// backward_kernel needs no statistics and streams.
+// bytes. Rows above 32 KB take wide_kernel, shorter ones narrow_kernel, and a
+// gradient whose row's statistics are known already takes backward_kernel, which
+// only streams. Figures are microseconds and the share of the measured copy rate
+// (6.8 TB/s) at the bytes that the call cannot do without, bf16 where nothing is said.
 //
 // Rows start at any element: 16-byte vectors are counted from the line that the
 // row's logits begin in, and the two vectors at the ends that a row shares with
@@ -698,11 +693,12 @@ __device__ __forceinline__ float teacher_loss(const TeacherList& list, int k, co
 // logit, of the whole slice and of each of up to kCells parts of it; b is about the
 // k-th largest of the former, and where a thread's largest of a part is not below b
 // (about k places) that thread's vectors of the part are read again, mostly from L2,
-// and what is not below b goes on a list: little more than k keys. One warp does all
-// this while the working warps are at the next rows, ranks the list by comparing all
-// with all, and one CTA's merges the cluster's. Where a list overflows (many equal
-// logits, rows in rising order) or too few threads have met any, it is made by
-// finding the k-th largest key by its digits.
+// and what is not below b goes on a list: little more than k keys. One helper warp
+// does all this while the working warps are at the next rows, ranks the list by
+// comparing all with all, and one CTA's merges the cluster's. Where a list overflows
+// (the largest logits side by side, or k near the number of threads) b is raised by
+// halving; where that finds none (many equal logits) the k-th largest key is found by
+// its digits (the 150 largest of 500x100000 side by side: 0.5 ms raised, 2.0 by digits).
 constexpr int kCells = 8;
 constexpr int kPlaces = 512;
 template <int THREADS, int SLOTS, int CELLS = 1>
@@ -1231,6 +1227,28 @@ __device__ __forceinline__ void teacher_rest(const RowArgs& a, int64_t i, const 
     __syncwarp();
 }
 
+// Rows above kNarrowBytes. Persistent: a cluster of 1 to 8 CTAs takes row after row,
+// each CTA a slice, which bulk copies bring chunk by chunk through a ring in shared
+// memory; so the ring's copies run ahead into the next rows and nothing waits for a
+// whole CTA. Eight warps take the slice's statistics (a running maximum and sums a
+// thread, joined by warp) and send them to every CTA of the cluster through
+// distributed shared memory. One of four helper warps, which looked up the row's own
+// values (token, weight, the teacher's shares, the vectors shared with its neighbours)
+// before its turn, joins them in the order of the warps, so that results do not depend
+// on timing, writes the row's results and leaves the gradient's coefficients. For the
+// gradient the slice comes through the ring once more, from L2: first passes are kept
+// there and the rows at work fit, so HBM reads a row once. Keeping slices in shared
+// memory instead was slower: what is held there is not ahead of the work.
+//
+// Bound by HBM (policy loss of 8192x131072 with 10% padding 656 us, 0.91; scoring
+// 4096x131072 147, 0.97; distillation of it 319, 0.94; fp32 policy loss of 2000x65537
+// 168, 0.87). Beside it: 32 exponentials an SM and clock, two passes of them for a
+// gradient (a third of its time), and in calls of few rounds what the last one
+// leaves idle (distillation loss of 1000x50001 fp16 in 3.3 rounds 25, 0.58) or, of
+// alternatives, the last rows' lists (64 of 1500x100003 fp32 128, 0.69). A call of a
+// few rows is a chain: first copy, exchange and coefficients, second pass, about 6 us.
+// Arithmetic is packed by two (fp32 pairs); by single operations it was slower.
+//
 // GRAD: a gradient is asked for. ENT: the entropy is (or is in the gradient). TOP: alternatives.
 template <typename T, int OP, bool GRAD, bool ENT, bool TOP>
 __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant__ RowArgs a, const __grid_constant__ Plan plan) {
@@ -1603,7 +1621,10 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
 // A row of at most kNarrowBytes is taken by TEAM warps on their own: the plain
 // loads of many rows a SM hide one another's latency, and a row's second reading
 // comes from L1 or L2. What a row costs in wide_kernel beside its elements (about
-// 1 us of a CTA: helpers, barriers, exchange) would be most of a short row's time.
+// 1 us of a CTA: helpers, barriers, exchange) would be most of a short row's time
+// (8192x4000, policy loss: 34 us here, more than twice that there); from 32 KB on
+// the ring's copies win. Bound by instruction issue: scoring of 8192x4000 14 us, 0.69,
+// its policy loss 34, 0.57, 20 alternatives 27, of 8192x8001 49, 64 of 3133x8765 34.
 constexpr int kNarrowWarps = 4;
 constexpr int kNarrowBytes = 32768;
 constexpr int kAloneTop = 24;  // alternatives that one warp's lanes give a bound for
@@ -1804,6 +1825,11 @@ __global__ void __launch_bounds__(kNarrowWarps * 32) narrow_kernel(const __grid_
 constexpr int kBackThreads = 256;
 constexpr int kBackVecs = 4;  // a thread's, all loaded before the first is used
 
+// The statistics come with the call, so a thread loads its vectors, all at once, and
+// writes their gradient; no thread waits for another. Bound by HBM: 4096x131072 with
+// 10% padding 305 us, 0.98; fp16 of 1000x50001, whose rows begin anywhere, 34, 0.84; 64
+// rows of 32000 2.6 (7 by calls: the host's).
+//
 // A CTA takes 1024 neighbouring vectors of a row, each warp 32 of every 256; of rows
 // shorter than that each warp 128 of a row (WARPS; 8192x1000 25 us by CTAs, 8 by
 // warps; 4096x131072 303 by CTAs, 313 by warps).

@@ -58,3 +58,33 @@ def test_each_attention_call_is_one_named_range(probe):
     assert lines[0] == "CODES [-1, -1, -1, -1]"       # metadata-only tree: TP_ERR_INVALID_ARG, after the range opened
     assert lines[1:] == ["push tp_decode_ex", "pop", "push tp_prefill", "pop", "push tp_decode_host", "pop",
                          "push tp_decode_noalloc", "pop"]
+
+
+CHILD_LOGITS = r"""
+import ctypes, sys
+sys.path.insert(0, sys.argv[1])
+import paper_2508_17445_gb300 as tp
+probe = ctypes.CDLL(sys.argv[2])
+probe.probe_log.restype = ctypes.c_char_p
+lib = tp.load_library()
+zero = ctypes.c_float(0)
+codes = [lib.tp_token_logprobs(None, None, None, None, None, 0, None, None, None),
+         lib.tp_token_logprobs_backward(None, None, None, None, None, None, None, 0, None),
+         lib.tp_policy_loss(None, None, None, None, None, zero, zero, zero, None, None, None, None, 0, None),
+         lib.tp_distill_loss(None, None, None, 0, 0, None, None, None, 0, None)]
+print("CODES", codes)
+print(probe.probe_log().decode(), end="")
+"""
+
+
+def test_each_call_on_logits_is_one_named_range(probe):
+    from paper_2508_17445_gb300 import build
+    build.build()
+    env = dict(os.environ, NVTX_INJECTION64_PATH=probe)
+    res = subprocess.run([sys.executable, "-c", CHILD_LOGITS, ROOT, probe], env=env, capture_output=True, text=True,
+                         timeout=120)
+    assert res.returncode == 0, res.stderr
+    lines = res.stdout.strip().splitlines()
+    assert lines[0] == "CODES [-1, -1, -1, -1]"       # no logits: TP_ERR_INVALID_ARG, after the range opened
+    names = ["tp_token_logprobs", "tp_token_logprobs_backward", "tp_policy_loss", "tp_distill_loss"]
+    assert lines[1:] == [x for n in names for x in ("push " + n, "pop")]
