@@ -8,7 +8,7 @@
 // would overflow in c x_j, and the row's largest terms lose nothing.
 //
 // All of it is bound by HBM: 8 to 20 operations an element against its 2 or 4
-// bytes. Rows above 32 KB take wide_kernel, shorter ones narrow_kernel, and a
+// bytes. Rows above 32 KB or so take wide_kernel, shorter ones narrow_kernel, and a
 // gradient whose row's statistics are known already takes backward_kernel, which
 // only streams. Figures are microseconds and the share of the measured copy rate
 // (6.8 TB/s) at the bytes that the call cannot do without, bf16 where nothing is said.
@@ -1227,7 +1227,7 @@ __device__ __forceinline__ void teacher_rest(const RowArgs& a, int64_t i, const 
     __syncwarp();
 }
 
-// Rows above kNarrowBytes. Persistent: a cluster of 1 to 8 CTAs takes row after row,
+// Rows above narrow_bytes(). Persistent: a cluster of 1 to 8 CTAs takes row after row,
 // each CTA a slice, which bulk copies bring chunk by chunk through a ring in shared
 // memory; so the ring's copies run ahead into the next rows and nothing waits for a
 // whole CTA. Eight warps take the slice's statistics (a running maximum and sums a
@@ -1618,18 +1618,28 @@ __global__ void __launch_bounds__(kThreads, 2) wide_kernel(const __grid_constant
 }
 
 // ------------------------------------------------------------- short rows --
-// A row of at most kNarrowBytes is taken by TEAM warps on their own: the plain
+// A row of at most narrow_bytes() is taken by TEAM warps on their own: the plain
 // loads of many rows a SM hide one another's latency, and a row's second reading
 // comes from L1 or L2. What a row costs in wide_kernel beside its elements (about
 // 1 us of a CTA: helpers, barriers, exchange) would be most of a short row's time
-// (8192x4000, policy loss: 34 us here, more than twice that there); from 32 KB on
-// the ring's copies win. Bound by instruction issue: scoring of 8192x4000 14 us, 0.69,
+// (8192x4000, policy loss: 33 us here, 81 there; scoring 14 and 37); in longer rows the
+// ring's copies win. Bound by instruction issue: scoring of 8192x4000 14 us, 0.69,
 // its policy loss 34, 0.57, 20 alternatives 27, of 8192x8001 49, 64 of 3133x8765 34.
 constexpr int kNarrowWarps = 4;
-constexpr int kNarrowBytes = 32768;
+
+// The largest row taken so, in bytes. Many rows of 16-bit logits: 48 KB, else 32, a gradient of few rows 20, as one row's
+// two readings by four warps are then a longer chain than a cluster's (us, wide_kernel / here: policy loss of 1200x24000
+// bf16 34 / 29, 2400x32000 66 / 75, 64x8000 6.3 / 5.6, 64x16000 6.1 / 7.3; distillation of 1200x24000 35 / 27; 20
+// alternatives of 4096x16000 54 / 48, 1200x24000 23 / 24; scoring 2048x16000 fp32 25 / 28).
+template <typename T>
+int narrow_bytes(int n, bool grad, bool top) {
+    if (grad && n < 304) return 20 << 10;
+    return sizeof(T) == 2 && !top && n >= 608 ? 48 << 10 : 32 << 10;
+}
 constexpr int kAloneTop = 24;  // alternatives that one warp's lanes give a bound for
 
-// KEPT: a row has at most four vectors a thread; it is read once and stays in registers.
+// KEPT: a row has at most four vectors a thread; it is read once and stays in registers (64x4000, policy loss 3.4 us, read
+// twice 3.8, distillation 5.1 and 5.8; equal where rows fill the GPU).
 template <typename T, int OP, bool GRAD, bool ENT, bool TOP, int TEAM, bool KEPT>
 __global__ void __launch_bounds__(kNarrowWarps * 32) narrow_kernel(const __grid_constant__ RowArgs a) {
     extern __shared__ __align__(16) uint8_t space[];
@@ -1992,7 +2002,7 @@ cudaError_t launch_narrow(const RowArgs& a, cudaStream_t s) {
 template <typename T, int OP, bool GRAD, bool ENT, bool TOP = false>
 cudaError_t launch_rows(const RowArgs& a, cudaStream_t s) {
     constexpr int E = Vec<T>::E;
-    if ((int64_t)a.vocab * (int)sizeof(T) <= kNarrowBytes) {
+    if ((int64_t)a.vocab * (int)sizeof(T) <= narrow_bytes<T>(a.n, GRAD, TOP)) {
         // One warp a row where it holds the row, or where there are rows enough for 32 warps an SM (us, one warp / four:
         // policy loss of 8192 rows of 8 KB 32 / 38, of 2500 15 / 12, distillation 44 / 52, 22 / 15). The bound of a warp's
         // lanes is too low for more than kAloneTop alternatives (8192x2000 fp32, 24: 27 / 34; 8192x4000 bf16, 32: 84 / 43).
