@@ -308,6 +308,20 @@ def test_alternatives_in_one_place(dtype, n, v):
         check_logprobs(x, tok, k)
 
 
+# either side of the row sizes and row counts at which another kernel takes over, rows at any place
+@pytest.mark.parametrize("n,v,dtype", [(610, 24570, "bf16"), (610, 24577, "f16"), (600, 16385, "bf16"), (303, 10241, "f16"), (305, 10240, "bf16"),
+                                       (304, 8193, "f32"), (20, 5120, "f32"), (20, 5121, "f32")])
+def test_kernel_boundaries(n, v, dtype):
+    x, tok, g = make(n, v, dtype, 3, 1)
+    tok[::7] = -1
+    a = torch.randn(n, generator=g, device=DEV)
+    check_logprobs(x, tok)
+    check_logprobs(x, tok, 20)
+    check_policy(x, tok, a, None, None, dtype, 0.8)
+    ids, teacher = teacher_of(x, 20, g)
+    check_distill(x, ids, teacher, None, dtype, 0.8, *rows_like(n, v, dtype, 1, 3))
+
+
 # masks by finite values that stay finite as x / T, with coefficients that take their product past fp32
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n,v", [(3, 700), (2100, 300), (3, 9001), (3, 40000)])
